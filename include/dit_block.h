@@ -383,6 +383,128 @@ dit_status dit_unpatchify_euler(const dit_model_config *cfg, const dit_varlen *v
                                 const float *latent, const void *v, const float *dt,
                                 float *latent_out, hipStream_t stream);
 
+/* ------------------------------------------ the paged 8-bit key/value cache */
+
+/* Keys and values that stay from step to step -- the text keys and values of
+ * every block, or the finished frames that a video continues -- in pages of
+ * 8-bit values.  Requests get pages as they are admitted and as they grow, in
+ * any order, and give them back one by one; block tables and lengths are
+ * device memory, so a captured step serves whichever requests they name.
+ *
+ * A pool holds, for each of n_blocks blocks, n_pages pages of page_tokens
+ * tokens x n_kv_heads heads.  The block table's row r lists the pages of
+ * request r: its token i lies in page table[r * max_pages + i / page_tokens].
+ *
+ * A value is a float8 e4m3 code (4 significant bits, largest 448) times a power
+ * of two, 2^(s - 127), with one scale byte s for each page and head, in
+ * k_scale / v_scale [n_blocks, n_pages, n_kv_heads].  The tokens of a page lie
+ * in groups of 32, in the order in which a matrix instruction takes them:
+ *   k [n_blocks, n_pages, n_kv_heads, page_tokens / 32, head_dim / 16, 32, 16]:
+ *     element (.., g, c, t, e) is token 32 g + t, channel 16 c + e;
+ *   v [n_blocks, n_pages, n_kv_heads, page_tokens / 32, 2, head_dim, 16]:
+ *     element (.., g, f, d, 4 i + j) is token 32 g + 8 i + 4 f + j, channel d.
+ * Offsets are 64-bit; a pool may hold up to 2^31 - 1 groups per block
+ * (n_pages * n_kv_heads * page_tokens / 32).
+ *
+ * Block tables, lengths and slot maps are read by the kernels and not checked
+ * on the host; no value in them makes a kernel leave its buffers.  A length
+ * below 0 counts as 0, one over the table's width or the call's bound as that;
+ * tokens on a page outside 0 .. n_pages - 1 are not there.  A page belongs to
+ * one request: entries of one slot map that name a page twice leave either's
+ * values in it. */
+typedef struct {
+  int n_blocks, n_pages, n_kv_heads;
+  int head_dim;             /* 64 or 128 */
+  int page_tokens;          /* 32, 64, 128 or 256 */
+  int max_pages;            /* width of the block table; max_pages * page_tokens < 2^31 */
+  int table_rows;           /* requests that the table and lens have room for */
+  void *k, *v;              /* device: pools */
+  uint8_t *k_scale, *v_scale;
+  int32_t *table;           /* device [table_rows, max_pages] */
+  int32_t *lens;            /* device [table_rows]: cached tokens of each request */
+} dit_kv_cache;
+
+/* Entries that a slot map needs for n_rows input rows of n_req requests:
+ * n_rows / page_tokens + 2 * n_req (0 if an argument is invalid). */
+size_t dit_cache_run_bound(int page_tokens, int n_req, int64_t n_rows);
+
+/* Gives the requests' new tokens their places: request r (row r of the table)
+ * holds lens_before[r] tokens (device; NULL: 0 each) and gets added[r] more
+ * (device), whose rows lie in the input from row r * rows_per_req (a padded
+ * batch; n_rows = n_req * rows_per_req) or, with rows_per_req 0, packed one
+ * request after another (n_rows: rows there are).  New pages come from
+ * free_pages (device [n_free]) in order, requests in order: a request whose
+ * new pages do not all fit gets none, nor does any later one that needs a page.
+ * Such a request is refused, and so is one with a negative length, more tokens
+ * than its table row holds or rows past the input; it keeps what it had.
+ * Written: the new pages' entries of cache->table (no other entry);
+ *   cache->lens[0 .. n_req): the lengths afterwards;
+ *   runs (device [n_runs, 4], n_runs >= dit_cache_run_bound): the slot map,
+ *     one entry {page, first input row, first place in the page, tokens} for
+ *     each page that gets tokens, then zeros (tokens 0: nothing to write);
+ *   counts (device [4]): pages taken, entries written, requests refused, tokens
+ *     placed.
+ * The pools are not touched, and k .. v_scale may be NULL.  What is written
+ * must not overlap what is read, cache->lens and lens_before included. */
+dit_status dit_cache_tables(const dit_kv_cache *cache, int n_req, const int32_t *lens_before,
+                            const int32_t *added, int rows_per_req, int64_t n_rows,
+                            const int32_t *free_pages, int n_free, int32_t *runs, int n_runs,
+                            int32_t *counts, hipStream_t stream);
+
+/* Writes the keys and values of a slot map's tokens to their places in one
+ * block's pages.  k, v: [n_rows, n_kv_heads * head_dim] (dtype) at row strides
+ * in elements; both may lie in one buffer.  The scale of a page that the entry
+ * begins (place 0) is the smallest power of two 2^e, e >= -100, for which no
+ * finite value of its tokens exceeds 448 * 2^e; an entry that continues a page
+ * leaves the scale or makes it larger, and then brings the page's earlier codes
+ * to it.  Codes are rounded to nearest, ties to even; infinities become NaN.
+ * Places behind the entry's tokens and all other pages keep their bytes. */
+dit_status dit_cache_store(const dit_kv_cache *cache, int block, const void *k, const void *v,
+                           int64_t k_row_stride, int64_t v_row_stride, int64_t n_rows,
+                           const int32_t *runs, int n_runs, dit_dtype dtype, hipStream_t stream);
+
+/* Attention of packed queries over the cache, non-causal: for request r (row r
+ * of the table) and head h, O = softmax(Q K^T * softmax_scale) V over the
+ * request's cached tokens, with query rows cu_q[r]..cu_q[r+1] (host array) and
+ * query head h on key/value head h / (n_heads / n_kv_heads).  q, o, strides and
+ * softmax_scale as for dit_attention_varlen; head_dim (64 or 128 in both
+ * dtypes) and n_kv_heads, a divisor of n_heads, are the cache's.  A request
+ * without tokens gets rows of zeros; table rows from n_req on are not read.
+ * max_len bounds the lengths (0: the table's width): longer requests are cut
+ * there, and the work is divided by it.  Few queries over many tokens divide
+ * the tokens among workgroups and join them in the workspace: ws holds
+ * dit_attention_cached_workspace_size bytes, 256-byte aligned (0 bytes: NULL
+ * will do), its contents are scratch, and calls that may overlap in time, or
+ * captured graphs that may, each need their own. */
+size_t dit_attention_cached_workspace_size(const dit_kv_cache *cache, const int32_t *cu_q, int n_req,
+                                           int n_heads, int max_len, dit_dtype dtype);
+dit_status dit_attention_cached(const dit_kv_cache *cache, int block, const void *q, void *o,
+                                int64_t q_row_stride, int64_t o_row_stride, const int32_t *cu_q,
+                                int n_req, int n_heads, int max_len, float softmax_scale,
+                                dit_dtype dtype, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* dit_text_kv into a cache with n_blocks pools of the model's heads: the text
+ * rows that runs names go to their places in every block's pages (from
+ * dit_cache_tables with n_rows = vl->cu_seqlens_txt[n_req]).  The workspace
+ * holds one block's keys and values in the config's dtype,
+ * dit_text_kv_cached_workspace_size bytes, 256-byte aligned. */
+size_t dit_text_kv_cached_workspace_size(const dit_model_config *cfg, const dit_varlen *vl);
+dit_status dit_text_kv_cached(const dit_model_config *cfg, const dit_model_weights *w,
+                              const dit_varlen *vl, const void *txt, const dit_kv_cache *cache,
+                              const int32_t *runs, int n_runs, void *ws, size_t ws_bytes,
+                              hipStream_t stream);
+
+/* dit_denoise_step with the text keys and values of a cache: request r of the
+ * batch attends to row r of the cache's table.  vl->cu_seqlens_txt is not read
+ * and may be NULL.  A captured step may be replayed for other prompts: the
+ * table and lens name them. */
+size_t dit_denoise_cached_workspace_size(const dit_model_config *cfg, const dit_varlen *vl,
+                                         const dit_kv_cache *cache);
+dit_status dit_denoise_step_cached(const dit_model_config *cfg, const dit_model_weights *w,
+                                   const dit_varlen *vl, const float *latent, const float *t,
+                                   const float *dt, const dit_kv_cache *cache, float *latent_out,
+                                   void *ws, size_t ws_bytes, hipStream_t stream);
+
 /* -------------------------------------------------------------- diagnostics */
 
 const char *dit_status_string(dit_status s);

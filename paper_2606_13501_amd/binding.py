@@ -115,6 +115,15 @@ class CMigEntry(ctypes.Structure):
                 ("dst_off", ctypes.c_int64 * MIG_MAX_DIMS), ("extent", ctypes.c_int64 * MIG_MAX_DIMS),
                 ("bytes", ctypes.c_int64)]
 
+
+class CKvCache(ctypes.Structure):
+    _fields_ = [("n_blocks", ctypes.c_int), ("n_pages", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("page_tokens", ctypes.c_int), ("max_pages", ctypes.c_int),
+                ("table_rows", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -130,6 +139,7 @@ def lib() -> ctypes.CDLL:
     PC, PW, PV = ctypes.POINTER(CConfig), ctypes.POINTER(CWeights), ctypes.POINTER(CVarlen)
     PI = ctypes.POINTER(ctypes.c_int32)
     PM, PMW = ctypes.POINTER(CModelConfig), ctypes.POINTER(CModelWeights)
+    PK = ctypes.POINTER(CKvCache)
     sig = {
         "dit_block_workspace_size": (sz, [PC, PV]),
         "dit_block_forward": (i32, [PC, PW, PV, vp, vp, vp, vp, vp, vp, sz, vp]),
@@ -149,6 +159,15 @@ def lib() -> ctypes.CDLL:
         "dit_denoise_step": (i32, [PM, PMW, PV, vp, vp, vp, vp, vp, vp, sz, vp]),
         "dit_patchify": (i32, [PM, PV, vp, vp, vp]),
         "dit_unpatchify_euler": (i32, [PM, PV, vp, vp, vp, vp, vp]),
+        "dit_cache_run_bound": (sz, [i32, i32, i64]),
+        "dit_cache_tables": (i32, [PK, i32, vp, vp, i32, i64, vp, i32, vp, i32, vp, vp]),
+        "dit_cache_store": (i32, [PK, i32, vp, vp, i64, i64, i64, vp, i32, i32, vp]),
+        "dit_attention_cached_workspace_size": (sz, [PK, PI, i32, i32, i32, i32]),
+        "dit_attention_cached": (i32, [PK, i32, vp, vp, i64, i64, PI, i32, i32, i32, f32, i32, vp, sz, vp]),
+        "dit_text_kv_cached_workspace_size": (sz, [PM, PV]),
+        "dit_text_kv_cached": (i32, [PM, PMW, PV, vp, PK, vp, i32, vp, sz, vp]),
+        "dit_denoise_cached_workspace_size": (sz, [PM, PV, PK]),
+        "dit_denoise_step_cached": (i32, [PM, PMW, PV, vp, vp, vp, PK, vp, vp, sz, vp]),
         "dit_simulate": (i32, [ctypes.POINTER(CSimConfig), ctypes.POINTER(CSimTrace), ctypes.POINTER(CSimResult)]),
         "dit_migration_plan": (i32, [ctypes.POINTER(CMigField), ctypes.POINTER(CMigEntry), i64,
                                      ctypes.POINTER(ctypes.c_int64)]),
@@ -179,7 +198,10 @@ def exported_symbols() -> Sequence[str]:
                         "dit_timestep_modulation_noalloc", "dit_attention_varlen",
                         "dit_adaln_modulate", "dit_layer_norm_affine", "dit_linear", "dit_qk_norm_rope",
                         "dit_gated_residual", "dit_text_kv_elems", "dit_text_kv", "dit_denoise_workspace_size",
-                        "dit_denoise_step", "dit_patchify", "dit_unpatchify_euler", "dit_simulate",
+                        "dit_denoise_step", "dit_patchify", "dit_unpatchify_euler", "dit_cache_run_bound",
+                        "dit_cache_tables", "dit_cache_store", "dit_attention_cached_workspace_size",
+                        "dit_attention_cached", "dit_text_kv_cached_workspace_size", "dit_text_kv_cached",
+                        "dit_denoise_cached_workspace_size", "dit_denoise_step_cached", "dit_simulate",
                         "dit_migration_plan", "dit_migration_execute", "dit_debug_gemm_tile_n", "dit_debug_gemm_plan",
                         "dit_debug_attention_split", "dit_debug_attention_shape", "dit_debug_attention_plan",
                         "dit_status_string",
@@ -436,6 +458,131 @@ def patchify(cfg: ModelConfig, vl: Varlen, latent, tokens, stream=None):
 def unpatchify_euler(cfg: ModelConfig, vl: Varlen, latent, v, dt, latent_out, stream=None):
     _check(lib().dit_unpatchify_euler(ctypes.byref(cfg.c), ctypes.byref(vl.c), _ptr(latent), _ptr(v), _ptr(dt),
                                       _ptr(latent_out), _stream(stream)), "dit_unpatchify_euler")
+
+
+# ------------------------------------------- the paged 8-bit key/value cache
+
+
+def _want(t, name, dtype, shape=None):
+    """The tensor's own layout is what the library reads: type and shape exact, dense."""
+    if t.dtype != dtype or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ' (not dense)'}, needed: dense "
+                         f"{dtype}{'' if shape is None else ' ' + str(tuple(shape))}")
+    return t
+
+
+class KvCache:
+    """Python view of dit_kv_cache; keeps its tensors alive.
+
+    k: uint8 [n_blocks, n_pages, n_kv_heads, page_tokens / 32, head_dim / 16, 32, 16]
+    v: uint8 [n_blocks, n_pages, n_kv_heads, page_tokens / 32, 2, head_dim, 16]
+    k_scale, v_scale: uint8 [n_blocks, n_pages, n_kv_heads]
+    table: int32 [table_rows, max_pages]; lens: int32 [table_rows]
+
+    The n_blocks axis may be left out (one block)."""
+
+    def __init__(self, k, v, k_scale, v_scale, table, lens):
+        lead = k.shape[:-4]
+        if len(lead) not in (2, 3) or len(table.shape) != 2:
+            raise ValueError(f"k of shape {tuple(k.shape)}, table of shape {tuple(table.shape)}")
+        groups, head_dim = k.shape[-4], 16 * k.shape[-3]
+        _want(k, "k", torch.uint8, (*lead, groups, head_dim // 16, 32, 16))
+        _want(v, "v", torch.uint8, (*lead, groups, 2, head_dim, 16))
+        _want(k_scale, "k_scale", torch.uint8, lead)
+        _want(v_scale, "v_scale", torch.uint8, lead)
+        _want(table, "table", torch.int32)
+        _want(lens, "lens", torch.int32, table.shape[:1])
+        self.k, self.v, self.k_scale, self.v_scale, self.table, self.lens = k, v, k_scale, v_scale, table, lens
+        self.c = CKvCache(lead[0] if len(lead) == 3 else 1, lead[-2], lead[-1], head_dim, 32 * groups, table.shape[1],
+                          table.shape[0], *(t.data_ptr() for t in (k, v, k_scale, v_scale, table, lens)))
+
+    @classmethod
+    def empty(cls, n_pages, n_kv_heads, head_dim, page_tokens, table_rows, max_pages, n_blocks=1, device="cuda"):
+        """A cache without tokens: zero pages, no table entries, lengths 0."""
+        g = page_tokens // 32
+        u8 = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)
+        lead = (n_blocks, n_pages, n_kv_heads)
+        return cls(u8(*lead, g, head_dim // 16, 32, 16), u8(*lead, g, 2, head_dim, 16), u8(*lead), u8(*lead),
+                   torch.full((table_rows, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(table_rows, dtype=torch.int32, device=device))
+
+
+def cache_run_bound(page_tokens: int, n_req: int, n_rows: int) -> int:
+    return int(lib().dit_cache_run_bound(int(page_tokens), int(n_req), int(n_rows)))
+
+
+def cache_tables(cache: KvCache, lens_before, added, free_pages, runs, counts, n_rows: int, rows_per_req: int = 0,
+                 stream=None):
+    """lens_before None: every request is new; free_pages None: no page is free."""
+    i32 = torch.int32
+    n = _want(added, "added", i32).numel()
+    _want(runs, "runs", i32, (runs.shape[0], 4))
+    _want(counts, "counts", i32, (4,))
+    if lens_before is not None:
+        _want(lens_before, "lens_before", i32, added.shape)
+    n_free = 0 if free_pages is None else _want(free_pages, "free_pages", i32).numel()
+    _check(lib().dit_cache_tables(ctypes.byref(cache.c), n, _ptr(lens_before), _ptr(added), int(rows_per_req), int(n_rows),
+                                  _ptr(free_pages), n_free, _ptr(runs), runs.shape[0], _ptr(counts), _stream(stream)),
+           "dit_cache_tables")
+
+
+def _rows_of(t, name, width):
+    if t.dim() != 2 or t.stride(1) != 1 or t.shape[1] < width:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}; needed: rows of {width} dense values")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def cache_store(cache: KvCache, k, v, runs, block: int = 0, stream=None):
+    """k, v: [rows, n_kv_heads * head_dim], of any row stride."""
+    width = cache.c.n_kv_heads * cache.c.head_dim
+    if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
+        raise ValueError(f"k is {k.dtype} with {k.shape[0]} rows, v {v.dtype} with {v.shape[0]}")
+    ks, vs = _rows_of(k, "k", width), _rows_of(v, "v", width)
+    _want(runs, "runs", torch.int32, (runs.shape[0], 4))
+    _check(lib().dit_cache_store(ctypes.byref(cache.c), int(block), _ptr(k), _ptr(v), ks, vs, k.shape[0], _ptr(runs),
+                                 runs.shape[0], dtype_code(k.dtype), _stream(stream)), "dit_cache_store")
+
+
+def attention_cached_workspace_size(cache: KvCache, cu_q, n_heads: int, dtype: torch.dtype, max_len: int = 0) -> int:
+    cq = _i32(cu_q)
+    return int(lib().dit_attention_cached_workspace_size(ctypes.byref(cache.c), _pi(cq), len(cq) - 1, int(n_heads),
+                                                         int(max_len), dtype_code(dtype)))
+
+
+def attention_cached(cache: KvCache, q, o, cu_q, n_heads: int, ws=None, block: int = 0, max_len: int = 0,
+                     softmax_scale=None, stream=None):
+    """softmax_scale None: the library's default, 1/sqrt(head_dim); ws as attention_cached_workspace_size says."""
+    cq = _i32(cu_q)
+    width = n_heads * cache.c.head_dim
+    if q.dtype != o.dtype or min(q.shape[0], o.shape[0]) < cq[-1]:
+        raise ValueError(f"q is {q.dtype} with {q.shape[0]} rows, o {o.dtype} with {o.shape[0]}, cu_q ends at {cq[-1]}")
+    qs, os_ = _rows_of(q, "q", width), _rows_of(o, "o", width)
+    _check(lib().dit_attention_cached(ctypes.byref(cache.c), int(block), _ptr(q), _ptr(o), qs, os_, _pi(cq), len(cq) - 1,
+                                      int(n_heads), int(max_len), 0.0 if softmax_scale is None else softmax_scale,
+                                      dtype_code(q.dtype), _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0,
+                                      _stream(stream)), "dit_attention_cached")
+
+
+def text_kv_cached_workspace_size(cfg: ModelConfig, vl: Varlen) -> int:
+    return int(lib().dit_text_kv_cached_workspace_size(ctypes.byref(cfg.c), ctypes.byref(vl.c)))
+
+
+def text_kv_cached(cfg: ModelConfig, w: ModelWeights, vl: Varlen, txt, cache: KvCache, runs, ws, stream=None):
+    _want(runs, "runs", torch.int32, (runs.shape[0], 4))
+    _check(lib().dit_text_kv_cached(ctypes.byref(cfg.c), ctypes.byref(w.c), ctypes.byref(vl.c), _ptr(txt),
+                                    ctypes.byref(cache.c), _ptr(runs), runs.shape[0], _ptr(ws),
+                                    ws.numel() * ws.element_size(), _stream(stream)), "dit_text_kv_cached")
+
+
+def denoise_cached_workspace_size(cfg: ModelConfig, vl: Varlen, cache: KvCache) -> int:
+    return int(lib().dit_denoise_cached_workspace_size(ctypes.byref(cfg.c), ctypes.byref(vl.c), ctypes.byref(cache.c)))
+
+
+def denoise_step_cached(cfg: ModelConfig, w: ModelWeights, vl: Varlen, latent, t, dt, cache: KvCache, latent_out, ws,
+                        stream=None):
+    _check(lib().dit_denoise_step_cached(ctypes.byref(cfg.c), ctypes.byref(w.c), ctypes.byref(vl.c), _ptr(latent), _ptr(t),
+                                         _ptr(dt), ctypes.byref(cache.c), _ptr(latent_out), _ptr(ws),
+                                         ws.numel() * ws.element_size(), _stream(stream)), "dit_denoise_step_cached")
 
 
 # ------------------------------------------------------------ the simulator

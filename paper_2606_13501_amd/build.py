@@ -16,7 +16,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libditblock.so")
 
-SOURCES = ["gemm.hip", "attention.hip", "rowwise.hip", "latent.hip", "api.cpp", "sim.cpp", "migrate.hip"]
+SOURCES = ["gemm.hip", "attention.hip", "rowwise.hip", "latent.hip", "cache.hip", "cached_attention.hip",
+           "api.cpp", "sim.cpp", "migrate.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + INCLUDE, "-I" + CSRC,
@@ -31,7 +32,7 @@ FLAGS = [
 # the padding), so its loops are aligned to 64 bytes and its speed no longer
 # depends on the size of the code in front of them.  The GEMM's timing does
 # not depend on loop alignment.
-EXTRA = {"attention.hip": ["-falign-loops=64"]}
+EXTRA = {"attention.hip": ["-falign-loops=64"], "cached_attention.hip": ["-falign-loops=64"]}
 
 
 def _compile(src: str) -> str:

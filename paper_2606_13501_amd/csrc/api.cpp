@@ -399,27 +399,37 @@ SideStream* side_stream() {
   return g_side[dev];
 }
 
+// One block's text keys and values in a paged cache, and the cached attention's workspace.
+struct CachedText {
+  const dit_kv_cache* cache;
+  int block;
+  void* ws;
+};
+CachedAttnArgs cached_args(const dit_kv_cache* c, int block, const void* q, void* o, int64_t qs, int64_t os,
+                           const ReqTable& cq, int n_heads, int max_len, float scale, dit_dtype dt);
+
 // S5..S12 on this GPU's rows given the self-attention output o.
 // With kv != NULL the text keys and values come from that cache ([txt_rows, 2D],
 // normalised keys) and txt is not read; kv_side != NULL: kv is still being
 // written on that side stream, whose join event s waits for before the
-// cross-attention (the caller holds its mutex).
+// cross-attention (the caller holds its mutex).  With cached != NULL they come
+// from that cache instead, and neither txt nor kv nor the text offsets are read.
 dit_status post_attention_impl(const dit_block_config* c, const dit_block_weights* w, const dit_varlen* vl,
                                const void* x, const void* o, const void* txt, const float* mod, void* y,
                                const Workspace& ws, hipStream_t s, const void* kv = nullptr,
-                               SideStream* kv_side = nullptr) {
+                               SideStream* kv_side = nullptr, const CachedText* cached = nullptr) {
   const int D = c->hidden, Dff = c->mlp_hidden;
   const int64_t T = vl->cu_seqlens[vl->n_req];
-  const int64_t L = vl->cu_seqlens_txt[vl->n_req];
+  const int64_t L = cached ? 0 : vl->cu_seqlens_txt[vl->n_req];
   const size_t es = elem_size(c->dtype);
   const ReqTable req = make_req(vl->cu_seqlens, vl->n_req);
-  const ReqTable req_txt = make_req(vl->cu_seqlens_txt, vl->n_req);
+  const ReqTable req_txt = cached ? single_req(0) : make_req(vl->cu_seqlens_txt, vl->n_req);
   const dit_dtype dt = c->dtype;
   // [ck | cv] = txt W_ckv^T + b_ckv ; ck = RMS(ck), on the side stream when there is one
   const char* ckv = (const char*)kv;
   SideStream* side = kv ? kv_side : nullptr;
   std::unique_lock<std::mutex> side_lock;
-  if (!ckv) {
+  if (!ckv && !cached) {
     side = side_stream();
     if (side) {
       side_lock = std::unique_lock<std::mutex>(side->mu);
@@ -448,9 +458,17 @@ dit_status post_attention_impl(const dit_block_config* c, const dit_block_weight
   }
   if (side) DIT_HIP(hipStreamWaitEvent(s, side->join, 0), "hipStreamWaitEvent");
   // oc = cross attention (queries: the request's latent rows, keys: its text rows)
-  DIT_TRY(run_attention(ws.cq, ckv, ckv + D * es, ws.o, D, 2 * D, 2 * D, D, req, req_txt, c->n_heads,
-                        c->head_dim, 1.0f / sqrtf((float)c->head_dim), dt, s,
-                        cq_norm_in_attn ? w->g_cq : nullptr, c->rms_eps));
+  if (cached) {
+    CachedAttnArgs p = cached_args(cached->cache, cached->block, ws.cq, ws.o, D, D, req, c->n_heads, 0,
+                                   1.0f / sqrtf((float)c->head_dim), dt);
+    p.q_gain = cq_norm_in_attn ? w->g_cq : nullptr;
+    p.q_eps = c->rms_eps;
+    DIT_HIP(launch_cached_attention(p, cached->ws, s), "cached attention");
+  } else {
+    DIT_TRY(run_attention(ws.cq, ckv, ckv + D * es, ws.o, D, 2 * D, 2 * D, D, req, req_txt, c->n_heads,
+                          c->head_dim, 1.0f / sqrtf((float)c->head_dim), dt, s,
+                          cq_norm_in_attn ? w->g_cq : nullptr, c->rms_eps));
+  }
   // x2 = x1 + (oc W_co^T + b_co), in place in x1
   DIT_TRY(run_linear(ws.o, D, w->w_co, D, w->b_co, ws.x1, D, T, D, D, DIT_EPI_RESIDUAL, ws.x1, D, nullptr, 0, req,
                      dt, s, "cross output projection"));
@@ -510,8 +528,8 @@ dit_status check_model_cfg(const dit_model_config* m) {
 }
 
 // Whole requests only; fills the latent geometry.
-dit_status check_model_varlen(const dit_model_config* m, const dit_varlen* vl, LatentTable* tab) {
-  DIT_TRY(check_varlen(vl, true));
+dit_status check_model_varlen(const dit_model_config* m, const dit_varlen* vl, LatentTable* tab, bool need_txt = true) {
+  DIT_TRY(check_varlen(vl, need_txt));
   if (!vl->grid_fhw) return fail(DIT_ERR_INVALID_ARG, "grid_fhw is NULL");
   memset(tab, 0, sizeof(*tab));
   tab->n_req = vl->n_req;
@@ -560,6 +578,18 @@ dit_status check_model_weights(const dit_model_config* m, const dit_model_weight
   return DIT_OK;
 }
 
+// The weights of every block's text key/value projection.
+dit_status check_text_weights(const dit_model_config* cfg, const dit_model_weights* w) {
+  if (!w || !w->blocks) return fail(DIT_ERR_INVALID_ARG, "model weights or their blocks are NULL");
+  for (int b = 0; b < cfg->n_blocks; ++b) {
+    const dit_block_weights* bw = &w->blocks[b];
+    if (check_ptr(bw->w_ckv, "w_ckv") != DIT_OK || check_ptr(bw->b_ckv, "b_ckv") != DIT_OK ||
+        check_ptr(bw->g_ck, "g_ck", !cfg->block.qk_norm) != DIT_OK)
+      return fail(DIT_ERR_INVALID_ARG, "block %d: %s", b, g_last_error.c_str());
+  }
+  return DIT_OK;
+}
+
 struct ModelWorkspace {
   char *x, *tok;
   Workspace blk;
@@ -600,6 +630,176 @@ dit_status run_cond_parts(const dit_block_config* c, int n_req, const float* t, 
   p.w_t1 = w_t1; p.b_t1 = b_t1; p.w_t2 = w_t2; p.b_t2 = b_t2; p.w_ada = w_mod; p.b_ada = b_mod; p.n_mod = n_mod;
   p.e = ws.e; p.a1 = ws.a1; p.c = ws.c; p.mod = mod; p.dtype = c->dtype;
   return hip_status(launch_conditioning(p, s), what);
+}
+
+// ------------------------------------------------ paged key/value cache
+
+size_t cache_page_bytes(const dit_kv_cache* c) { return (size_t)c->n_kv_heads * c->page_tokens * c->head_dim; }
+
+// The sizes, and the parts that a call uses: pools (pages and scales), the table.
+dit_status check_cache(const dit_kv_cache* c, bool pools, int n_req) {
+  if (!c) return fail(DIT_ERR_INVALID_ARG, "cache is NULL");
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(DIT_ERR_UNSUPPORTED, "cache head_dim %d (64 or 128)", c->head_dim);
+  if (c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128 && c->page_tokens != 256)
+    return fail(DIT_ERR_UNSUPPORTED, "cache page of %d tokens (32, 64, 128 or 256)", c->page_tokens);
+  if (c->n_blocks < 1 || c->n_pages < 1 || c->n_kv_heads < 1)
+    return fail(DIT_ERR_INVALID_ARG, "cache of %d blocks, %d pages, %d heads", c->n_blocks, c->n_pages, c->n_kv_heads);
+  const double groups = (double)c->n_pages * c->n_kv_heads * (c->page_tokens / 32);
+  if (groups > 2147483647.0) return fail(DIT_ERR_UNSUPPORTED, "cache of %.0f groups of 32 tokens per block (at most 2^31 - 1)", groups);
+  if (pools) {
+    DIT_TRY(check_ptr(c->k, "cache k")); DIT_TRY(check_ptr(c->v, "cache v"));
+    DIT_TRY(check_ptr(c->k_scale, "cache k_scale")); DIT_TRY(check_ptr(c->v_scale, "cache v_scale"));
+  }
+  if (n_req > 0) {
+    if (c->max_pages < 1 || (int64_t)c->max_pages * c->page_tokens > 0x7FFFFFFF)
+      return fail(DIT_ERR_INVALID_ARG, "cache table of %d pages of %d tokens per request", c->max_pages, c->page_tokens);
+    if (n_req > c->table_rows) return fail(DIT_ERR_INVALID_ARG, "%d requests, the cache table has %d rows", n_req, c->table_rows);
+    DIT_TRY(check_ptr(c->table, "cache table")); DIT_TRY(check_ptr(c->lens, "cache lens"));
+  }
+  return DIT_OK;
+}
+
+dit_status check_cache_block(const dit_kv_cache* c, int block) {
+  if (block < 0 || block >= c->n_blocks) return fail(DIT_ERR_INVALID_ARG, "block %d of a cache of %d", block, c->n_blocks);
+  return DIT_OK;
+}
+
+int log2_of(int v) {
+  int s = 0;
+  while ((1 << s) < v) ++s;
+  return s;
+}
+
+dit_status run_cache_store(const dit_kv_cache* c, int block, const void* k, const void* v, int64_t ks, int64_t vs,
+                           int64_t n_rows, const int32_t* runs, int n_runs, dit_dtype dt, hipStream_t s) {
+  CacheStoreArgs p;
+  p.k = k; p.v = v; p.k_stride = ks; p.v_stride = vs; p.n_rows = n_rows; p.runs = runs;
+  const size_t pages = (size_t)block * c->n_pages;
+  p.k_pages = (char*)c->k + pages * cache_page_bytes(c);
+  p.v_pages = (char*)c->v + pages * cache_page_bytes(c);
+  p.k_scale = c->k_scale + pages * c->n_kv_heads;
+  p.v_scale = c->v_scale + pages * c->n_kv_heads;
+  p.n_pages = c->n_pages; p.n_kv_heads = c->n_kv_heads; p.head_dim = c->head_dim; p.page_tokens = c->page_tokens;
+  p.dtype = dt;
+  return hip_status(launch_cache_store(p, n_runs, s), "cache store");
+}
+
+// The kernels' arguments; max_len 0: the table's width.
+CachedAttnArgs cached_args(const dit_kv_cache* c, int block, const void* q, void* o, int64_t qs, int64_t os,
+                           const ReqTable& cq, int n_heads, int max_len, float scale, dit_dtype dt) {
+  CachedAttnArgs p;
+  p.q = q; p.o = o; p.q_stride = qs; p.o_stride = os; p.cq = cq;
+  p.n_heads = n_heads; p.n_kv_heads = c->n_kv_heads; p.head_dim = c->head_dim;
+  const size_t pages = (size_t)block * c->n_pages;
+  p.k_pages = (const char*)c->k + pages * cache_page_bytes(c);
+  p.v_pages = (const char*)c->v + pages * cache_page_bytes(c);
+  p.k_scale = c->k_scale + pages * c->n_kv_heads;
+  p.v_scale = c->v_scale + pages * c->n_kv_heads;
+  p.table = c->table; p.lens = c->lens;
+  p.n_pages = c->n_pages; p.page_shift = log2_of(c->page_tokens); p.max_pages = c->max_pages;
+  const int width = c->max_pages * c->page_tokens;
+  p.max_len = max_len > 0 && max_len < width ? max_len : width;
+  p.scale = scale; p.dtype = dt;
+  return p;
+}
+
+// Work items (128 query rows of a key/value head or fewer, up to 64 key pieces
+// each) are numbered in 23 bits: a launch of fewer than 2^32 work-items.
+dit_status check_cached_items(const dit_kv_cache* c, const int32_t* cu, int n_req, int n_heads, dit_dtype dt) {
+  const int64_t group = n_heads / c->n_kv_heads, rows = dt == DIT_F32 ? 16 : 128;
+  int64_t items = 0;
+  for (int r = 0; r < n_req; ++r) items += ((cu[r + 1] - cu[r]) * group + rows - 1) / rows * c->n_kv_heads;
+  if (items > (1 << 23)) return fail(DIT_ERR_UNSUPPORTED, "cached attention of %lld work items (at most 2^23)", (long long)items);
+  return DIT_OK;
+}
+
+dit_status check_cached_heads(const dit_kv_cache* c, int n_heads) {
+  if (n_heads < 1 || n_heads % c->n_kv_heads)
+    return fail(DIT_ERR_INVALID_ARG, "%d query heads over %d key/value heads", n_heads, c->n_kv_heads);
+  return DIT_OK;
+}
+
+// A cache that serves a model: its heads, one pool per block, its dtype's head size.
+dit_status check_model_cache(const dit_model_config* m, const dit_kv_cache* c, int n_req) {
+  DIT_TRY(check_cache(c, true, n_req));
+  if (c->n_kv_heads != m->block.n_heads || c->head_dim != m->block.head_dim)
+    return fail(DIT_ERR_INVALID_ARG, "cache of %d heads of %d, the model has %d of %d", c->n_kv_heads, c->head_dim,
+                m->block.n_heads, m->block.head_dim);
+  if (c->n_blocks != m->n_blocks) return fail(DIT_ERR_INVALID_ARG, "cache of %d blocks, the model has %d", c->n_blocks, m->n_blocks);
+  return DIT_OK;
+}
+
+// Workspace of the cross-attention of a cached step, behind the step's own.
+size_t cached_step_ws(const dit_model_config* m, const dit_varlen* vl, const dit_kv_cache* cache) {
+  const dit_block_config* c = &m->block;
+  return round256(cached_attention_ws(cached_args(cache, 0, nullptr, nullptr, 0, 0, make_req(vl->cu_seqlens, vl->n_req),
+                                                  c->n_heads, 0, 1.f, c->dtype)));
+}
+
+// One step with the text keys and values of kv, or with cache != NULL those of the cache.
+dit_status denoise_step_impl(const dit_model_config* cfg, const dit_model_weights* w, const dit_varlen* vl,
+                             const float* latent, const float* t, const float* dt, const void* kv,
+                             const dit_kv_cache* cache, float* latent_out, void* ws, size_t ws_bytes,
+                             hipStream_t stream) {
+  DIT_TRY(check_model_cfg(cfg));
+  LatentTable tab;
+  DIT_TRY(check_model_varlen(cfg, vl, &tab, !cache));
+  DIT_TRY(check_model_weights(cfg, w));
+  const dit_block_config* c = &cfg->block;
+  RopeTable rope;
+  DIT_TRY(check_rope_table(vl, c->rope_sections, &rope));
+  DIT_TRY(check_attn_items(vl->cu_seqlens, vl->n_req, c->n_heads));
+  DIT_TRY(check_ptr(latent, "latent")); DIT_TRY(check_ptr(t, "t")); DIT_TRY(check_ptr(dt, "dt"));
+  if (cache) {
+    DIT_TRY(check_model_cache(cfg, cache, vl->n_req));
+    DIT_TRY(check_cached_items(cache, vl->cu_seqlens, vl->n_req, c->n_heads, c->dtype));
+  } else {
+    DIT_TRY(check_ptr(kv, "kv"));
+  }
+  DIT_TRY(check_ptr(latent_out, "latent_out"));
+  const size_t own = model_layout(cfg, vl, nullptr, nullptr);
+  const size_t need = own + (cache ? cached_step_ws(cfg, vl, cache) : 0);
+  if (!ws) return fail(DIT_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
+  if (((uintptr_t)ws & 255u) != 0) return fail(DIT_ERR_WORKSPACE, "workspace is not 256-byte aligned");
+  if (ws_bytes < need) return fail(DIT_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
+  ModelWorkspace W;
+  model_layout(cfg, vl, (char*)ws, &W);
+
+  const int D = c->hidden, P = patch_len(cfg), R = vl->n_req;
+  const int64_t T = vl->cu_seqlens[R], L = cache ? 0 : vl->cu_seqlens_txt[R];
+  const size_t es = elem_size(c->dtype);
+  const dit_dtype dty = c->dtype;
+  const ReqTable req = make_req(vl->cu_seqlens, R);
+  // x = patchify(latent) W_pe^T + b_pe
+  DIT_TRY(run_latent(false, cfg, tab, latent, W.tok, nullptr, nullptr, stream));
+  DIT_TRY(run_linear(W.tok, P, w->w_pe, P, w->b_pe, W.x, D, T, D, P, DIT_EPI_NONE, nullptr, 0, nullptr, 0, req, dty,
+                     stream, "patch embedding"));
+  // SiLU(c) of the shared timestep MLP, once for all blocks
+  DIT_TRY(run_cond_parts(c, R, t, w->w_t1, w->b_t1, w->w_t2, w->b_t2, nullptr, nullptr, 0, nullptr, W.blk, stream,
+                         "timestep MLP"));
+  const Workspace& B = W.blk;
+  for (int b = 0; b < cfg->n_blocks; ++b) {
+    const dit_block_weights* bw = &w->blocks[b];
+    DIT_TRY(run_cond_parts(c, R, t, nullptr, nullptr, nullptr, nullptr, bw->w_ada, bw->b_ada, 6, B.mod, B, stream,
+                           "block modulation"));
+    DIT_TRY(pre_attention_impl(c, bw, vl, W.x, B.mod, B.qkv, B, stream));
+    DIT_TRY(self_attention_impl(c, vl, B.qkv, B.o, stream));
+    if (cache) {
+      const CachedText ct = {cache, b, (char*)ws + own};
+      DIT_TRY(post_attention_impl(c, bw, vl, W.x, B.o, nullptr, B.mod, W.x, B, stream, nullptr, nullptr, &ct));
+    } else {
+      DIT_TRY(post_attention_impl(c, bw, vl, W.x, B.o, nullptr, B.mod, W.x, B, stream,
+                                  (const char*)kv + (size_t)b * L * 2 * D * es));
+    }
+  }
+  // output layer: v = (LN(x)(1 + scale) + shift) W_out^T + b_out with (shift, scale) = W_hmod SiLU(c) + b_hmod
+  DIT_TRY(run_cond_parts(c, R, t, nullptr, nullptr, nullptr, nullptr, w->w_hmod, w->b_hmod, 2, B.mod, B, stream,
+                         "output modulation"));
+  DIT_TRY(run_ln_mod(W.x, B.mod, B.mod + D, 2 * D, req, T, D, c->ln_eps, B.h, dty, stream));
+  DIT_TRY(run_linear(B.h, D, w->w_out, D, w->b_out, W.tok, P, T, P, D, DIT_EPI_NONE, nullptr, 0, nullptr, 0, req, dty,
+                     stream, "output projection"));
+  // latent_out = latent + dt * unpatchify(v)
+  return run_latent(true, cfg, tab, latent, W.tok, dt, latent_out, stream);
 }
 
 }  // namespace
@@ -999,14 +1199,8 @@ dit_status dit_text_kv(const dit_model_config* cfg, const dit_model_weights* w, 
   g_last_error.clear();
   DIT_TRY(check_model_cfg(cfg));
   DIT_TRY(check_varlen(vl, true));
-  if (!w || !w->blocks) return fail(DIT_ERR_INVALID_ARG, "model weights or their blocks are NULL");
+  DIT_TRY(check_text_weights(cfg, w));
   const dit_block_config* c = &cfg->block;
-  for (int b = 0; b < cfg->n_blocks; ++b) {
-    const dit_block_weights* bw = &w->blocks[b];
-    if (check_ptr(bw->w_ckv, "w_ckv") != DIT_OK || check_ptr(bw->b_ckv, "b_ckv") != DIT_OK ||
-        check_ptr(bw->g_ck, "g_ck", !c->qk_norm) != DIT_OK)
-      return fail(DIT_ERR_INVALID_ARG, "block %d: %s", b, g_last_error.c_str());
-  }
   DIT_TRY(check_ptr(txt, "txt"));
   DIT_TRY(check_ptr(kv, "kv"));
   const int64_t L = vl->cu_seqlens_txt[vl->n_req];
@@ -1027,53 +1221,172 @@ dit_status dit_denoise_step(const dit_model_config* cfg, const dit_model_weights
                             const float* latent, const float* t, const float* dt, const void* kv, float* latent_out,
                             void* ws, size_t ws_bytes, hipStream_t stream) {
   g_last_error.clear();
-  DIT_TRY(check_model_cfg(cfg));
-  LatentTable tab;
-  DIT_TRY(check_model_varlen(cfg, vl, &tab));
-  DIT_TRY(check_model_weights(cfg, w));
-  const dit_block_config* c = &cfg->block;
-  RopeTable rope;
-  DIT_TRY(check_rope_table(vl, c->rope_sections, &rope));
-  DIT_TRY(check_attn_items(vl->cu_seqlens, vl->n_req, c->n_heads));
-  DIT_TRY(check_ptr(latent, "latent")); DIT_TRY(check_ptr(t, "t")); DIT_TRY(check_ptr(dt, "dt"));
-  DIT_TRY(check_ptr(kv, "kv")); DIT_TRY(check_ptr(latent_out, "latent_out"));
-  const size_t need = model_layout(cfg, vl, nullptr, nullptr);
-  if (!ws) return fail(DIT_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
-  if (((uintptr_t)ws & 255u) != 0) return fail(DIT_ERR_WORKSPACE, "workspace is not 256-byte aligned");
-  if (ws_bytes < need) return fail(DIT_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
-  ModelWorkspace W;
-  model_layout(cfg, vl, (char*)ws, &W);
+  return denoise_step_impl(cfg, w, vl, latent, t, dt, kv, nullptr, latent_out, ws, ws_bytes, stream);
+}
 
-  const int D = c->hidden, P = patch_len(cfg), R = vl->n_req;
-  const int64_t T = vl->cu_seqlens[R], L = vl->cu_seqlens_txt[R];
-  const size_t es = elem_size(c->dtype);
-  const dit_dtype dty = c->dtype;
-  const ReqTable req = make_req(vl->cu_seqlens, R);
-  // x = patchify(latent) W_pe^T + b_pe
-  DIT_TRY(run_latent(false, cfg, tab, latent, W.tok, nullptr, nullptr, stream));
-  DIT_TRY(run_linear(W.tok, P, w->w_pe, P, w->b_pe, W.x, D, T, D, P, DIT_EPI_NONE, nullptr, 0, nullptr, 0, req, dty,
-                     stream, "patch embedding"));
-  // SiLU(c) of the shared timestep MLP, once for all blocks
-  DIT_TRY(run_cond_parts(c, R, t, w->w_t1, w->b_t1, w->w_t2, w->b_t2, nullptr, nullptr, 0, nullptr, W.blk, stream,
-                         "timestep MLP"));
-  const Workspace& B = W.blk;
-  for (int b = 0; b < cfg->n_blocks; ++b) {
-    const dit_block_weights* bw = &w->blocks[b];
-    DIT_TRY(run_cond_parts(c, R, t, nullptr, nullptr, nullptr, nullptr, bw->w_ada, bw->b_ada, 6, B.mod, B, stream,
-                           "block modulation"));
-    DIT_TRY(pre_attention_impl(c, bw, vl, W.x, B.mod, B.qkv, B, stream));
-    DIT_TRY(self_attention_impl(c, vl, B.qkv, B.o, stream));
-    DIT_TRY(post_attention_impl(c, bw, vl, W.x, B.o, nullptr, B.mod, W.x, B, stream,
-                                (const char*)kv + (size_t)b * L * 2 * D * es));
+size_t dit_cache_run_bound(int page_tokens, int n_req, int64_t n_rows) {
+  if (page_tokens < 1 || n_req < 1 || n_req > DIT_MAX_REQ || n_rows < 0 || n_rows > 0x7FFFFFFF) return 0;
+  return (size_t)(n_rows / page_tokens) + 2 * (size_t)n_req;
+}
+
+dit_status dit_cache_tables(const dit_kv_cache* cache, int n_req, const int32_t* lens_before, const int32_t* added,
+                            int rows_per_req, int64_t n_rows, const int32_t* free_pages, int n_free, int32_t* runs,
+                            int n_runs, int32_t* counts, hipStream_t stream) {
+  g_last_error.clear();
+  if (n_req < 1 || n_req > DIT_MAX_REQ) return fail(DIT_ERR_INVALID_ARG, "n_req = %d outside 1..%d", n_req, DIT_MAX_REQ);
+  DIT_TRY(check_cache(cache, false, n_req));
+  DIT_TRY(check_ptr(lens_before, "lens_before", true)); DIT_TRY(check_ptr(added, "added"));
+  if (n_free < 0) return fail(DIT_ERR_INVALID_ARG, "n_free = %d", n_free);
+  DIT_TRY(check_ptr(free_pages, "free_pages", n_free == 0));
+  DIT_TRY(check_ptr(runs, "runs")); DIT_TRY(check_ptr(counts, "counts"));
+  if (n_rows < 0 || n_rows > 0x7FFFFFFF) return fail(DIT_ERR_INVALID_ARG, "n_rows %lld", (long long)n_rows);
+  if (rows_per_req < 0 || (rows_per_req > 0 && n_rows != (int64_t)n_req * rows_per_req))
+    return fail(DIT_ERR_INVALID_ARG, "rows_per_req = %d: a padded batch of %d requests has %d rows each, n_rows is %lld",
+                rows_per_req, n_req, rows_per_req, (long long)n_rows);
+  const size_t need = dit_cache_run_bound(cache->page_tokens, n_req, n_rows);
+  if (n_runs < 0 || (size_t)n_runs < need)
+    return fail(DIT_ERR_INVALID_ARG, "slot map of %d entries, %zu needed", n_runs, need);
+  const Span out[4] = {span(cache->table, n_req, cache->max_pages, cache->max_pages, 4), span(cache->lens, 1, 0, n_req, 4),
+                       span(runs, n_runs, 4, 4, 4), span(counts, 1, 0, 4, 4)};
+  const Span in[3] = {span(lens_before, lens_before ? 1 : 0, 0, n_req, 4), span(added, 1, 0, n_req, 4),
+                      span(free_pages, n_free > 0 ? 1 : 0, 0, n_free, 4)};
+  const char* names[7] = {"cache table", "cache lens", "runs", "counts", "lens_before", "added", "free_pages"};
+  for (int i = 0; i < 4; ++i)
+    for (int j = i + 1; j < 7; ++j)
+      if (overlaps(out[i], j < 4 ? out[j] : in[j - 4])) return fail(DIT_ERR_INVALID_ARG, "%s overlaps %s", names[i], names[j]);
+  CacheTablesArgs p;
+  p.n_req = n_req; p.page_shift = log2_of(cache->page_tokens); p.max_pages = cache->max_pages;
+  p.rows_per_req = rows_per_req; p.n_rows = (int)n_rows; p.n_free = n_free; p.n_runs = n_runs;
+  p.lens_before = lens_before; p.added = added; p.free_pages = free_pages;
+  p.table = cache->table; p.lens = cache->lens; p.runs = runs; p.counts = counts;
+  return hip_status(launch_cache_tables(p, stream), "cache tables");
+}
+
+dit_status dit_cache_store(const dit_kv_cache* cache, int block, const void* k, const void* v, int64_t k_row_stride,
+                           int64_t v_row_stride, int64_t n_rows, const int32_t* runs, int n_runs, dit_dtype dtype,
+                           hipStream_t stream) {
+  g_last_error.clear();
+  DIT_TRY(check_dtype(dtype));
+  DIT_TRY(check_cache(cache, true, 0));
+  DIT_TRY(check_cache_block(cache, block));
+  DIT_TRY(check_ptr(k, "k")); DIT_TRY(check_ptr(v, "v"));
+  if (n_rows < 0 || n_rows > 0x7FFFFFFF) return fail(DIT_ERR_INVALID_ARG, "n_rows %lld", (long long)n_rows);
+  if (n_runs < 0) return fail(DIT_ERR_INVALID_ARG, "slot map of %d entries", n_runs);
+  DIT_TRY(check_ptr(runs, "runs", n_runs == 0));
+  const int64_t width = (int64_t)cache->n_kv_heads * cache->head_dim, vec = dtype == DIT_BF16 ? 8 : 4;
+  if (k_row_stride < width || v_row_stride < width || k_row_stride % vec || v_row_stride % vec)
+    return fail(DIT_ERR_INVALID_ARG, "row stride %lld / %lld: must be >= n_kv_heads*head_dim = %lld and a multiple of %lld",
+                (long long)k_row_stride, (long long)v_row_stride, (long long)width, (long long)vec);
+  if ((int64_t)n_runs * 2 * cache->n_kv_heads > 0x7FFFFFFF)
+    return fail(DIT_ERR_UNSUPPORTED, "slot map of %d entries x %d heads", n_runs, cache->n_kv_heads);
+  const int64_t es = (int64_t)elem_size(dtype), pages = cache->n_pages, bytes = (int64_t)cache_page_bytes(cache);
+  const Span out[4] = {span((char*)cache->k + block * pages * bytes, pages, bytes, bytes, 1),
+                       span((char*)cache->v + block * pages * bytes, pages, bytes, bytes, 1),
+                       span(cache->k_scale + block * pages * cache->n_kv_heads, pages, cache->n_kv_heads, cache->n_kv_heads, 1),
+                       span(cache->v_scale + block * pages * cache->n_kv_heads, pages, cache->n_kv_heads, cache->n_kv_heads, 1)};
+  const Span in[3] = {span(k, n_rows, k_row_stride, width, es), span(v, n_rows, v_row_stride, width, es),
+                      span(runs, n_runs, 4, 4, 4)};
+  const char* names[7] = {"cache k", "cache v", "cache k_scale", "cache v_scale", "k", "v", "runs"};
+  for (int i = 0; i < 4; ++i)
+    for (int j = i + 1; j < 7; ++j)
+      if (overlaps(out[i], j < 4 ? out[j] : in[j - 4])) return fail(DIT_ERR_INVALID_ARG, "%s overlaps %s", names[i], names[j]);
+  return run_cache_store(cache, block, k, v, k_row_stride, v_row_stride, n_rows, runs, n_runs, dtype, stream);
+}
+
+size_t dit_attention_cached_workspace_size(const dit_kv_cache* cache, const int32_t* cu_q, int n_req, int n_heads,
+                                           int max_len, dit_dtype dtype) {
+  if (check_dtype(dtype) != DIT_OK || check_cu(cu_q, n_req, "cu_q") != DIT_OK || check_cache(cache, false, n_req) != DIT_OK ||
+      check_cached_heads(cache, n_heads) != DIT_OK || max_len < 0 ||
+      check_cached_items(cache, cu_q, n_req, n_heads, dtype) != DIT_OK)
+    return 0;
+  return cached_attention_ws(cached_args(cache, 0, nullptr, nullptr, 0, 0, make_req(cu_q, n_req), n_heads, max_len, 1.f, dtype));
+}
+
+dit_status dit_attention_cached(const dit_kv_cache* cache, int block, const void* q, void* o, int64_t q_row_stride,
+                                int64_t o_row_stride, const int32_t* cu_q, int n_req, int n_heads, int max_len,
+                                float softmax_scale, dit_dtype dtype, void* ws, size_t ws_bytes, hipStream_t stream) {
+  g_last_error.clear();
+  DIT_TRY(check_dtype(dtype));
+  DIT_TRY(check_cu(cu_q, n_req, "cu_q"));
+  DIT_TRY(check_cache(cache, true, n_req));
+  DIT_TRY(check_cache_block(cache, block));
+  DIT_TRY(check_cached_heads(cache, n_heads));
+  DIT_TRY(check_ptr(q, "q")); DIT_TRY(check_ptr(o, "o"));
+  if (max_len < 0) return fail(DIT_ERR_INVALID_ARG, "max_len = %d", max_len);
+  if (!isfinite(softmax_scale)) return fail(DIT_ERR_INVALID_ARG, "softmax_scale is not finite");
+  const float scale = softmax_scale == 0.f ? 1.0f / sqrtf((float)cache->head_dim) : softmax_scale;
+  const int64_t width = (int64_t)n_heads * cache->head_dim, vec = dtype == DIT_BF16 ? 8 : 4;
+  if (q_row_stride < width || o_row_stride < width || q_row_stride % vec || o_row_stride % vec)
+    return fail(DIT_ERR_INVALID_ARG, "row stride %lld / %lld: must be >= n_heads*head_dim = %lld and a multiple of %lld",
+                (long long)q_row_stride, (long long)o_row_stride, (long long)width, (long long)vec);
+  DIT_TRY(check_cached_items(cache, cu_q, n_req, n_heads, dtype));
+  const CachedAttnArgs p = cached_args(cache, block, q, o, q_row_stride, o_row_stride, make_req(cu_q, n_req), n_heads,
+                                       max_len, scale, dtype);
+  const size_t need = cached_attention_ws(p);
+  if (need > 0) {
+    if (!ws || ((uintptr_t)ws & 255u)) return fail(DIT_ERR_WORKSPACE, "workspace NULL or not 256-byte aligned (%zu bytes needed)", need);
+    if (ws_bytes < need) return fail(DIT_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
   }
-  // output layer: v = (LN(x)(1 + scale) + shift) W_out^T + b_out with (shift, scale) = W_hmod SiLU(c) + b_hmod
-  DIT_TRY(run_cond_parts(c, R, t, nullptr, nullptr, nullptr, nullptr, w->w_hmod, w->b_hmod, 2, B.mod, B, stream,
-                         "output modulation"));
-  DIT_TRY(run_ln_mod(W.x, B.mod, B.mod + D, 2 * D, req, T, D, c->ln_eps, B.h, dty, stream));
-  DIT_TRY(run_linear(B.h, D, w->w_out, D, w->b_out, W.tok, P, T, P, D, DIT_EPI_NONE, nullptr, 0, nullptr, 0, req, dty,
-                     stream, "output projection"));
-  // latent_out = latent + dt * unpatchify(v)
-  return run_latent(true, cfg, tab, latent, W.tok, dt, latent_out, stream);
+  // o and the workspace are written while everything else is read
+  const int64_t es = (int64_t)elem_size(dtype), pages = cache->n_pages, bytes = (int64_t)cache_page_bytes(cache);
+  const Span out[2] = {span(o, cu_q[n_req], o_row_stride, width, es), span(ws, need > 0 ? 1 : 0, 0, (int64_t)need, 1)};
+  const Span in[7] = {span(q, cu_q[n_req], q_row_stride, width, es), span(p.k_pages, pages, bytes, bytes, 1),
+                      span(p.v_pages, pages, bytes, bytes, 1), span(p.k_scale, pages, cache->n_kv_heads, cache->n_kv_heads, 1),
+                      span(p.v_scale, pages, cache->n_kv_heads, cache->n_kv_heads, 1),
+                      span(cache->table, n_req, cache->max_pages, cache->max_pages, 4), span(cache->lens, 1, 0, n_req, 4)};
+  const char* names[7] = {"q", "cache k", "cache v", "cache k_scale", "cache v_scale", "cache table", "cache lens"};
+  if (overlaps(out[0], out[1])) return fail(DIT_ERR_INVALID_ARG, "o overlaps the workspace");
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 7; ++j)
+      if (overlaps(out[i], in[j])) return fail(DIT_ERR_INVALID_ARG, "%s overlaps %s", i ? "the workspace" : "o", names[j]);
+  return hip_status(launch_cached_attention(p, ws, stream), "cached attention");
+}
+
+size_t dit_text_kv_cached_workspace_size(const dit_model_config* cfg, const dit_varlen* vl) {
+  if (check_model_cfg(cfg) != DIT_OK || check_varlen(vl, true) != DIT_OK) return 0;
+  return round256((size_t)vl->cu_seqlens_txt[vl->n_req] * 2 * cfg->block.hidden * elem_size(cfg->block.dtype));
+}
+
+dit_status dit_text_kv_cached(const dit_model_config* cfg, const dit_model_weights* w, const dit_varlen* vl,
+                              const void* txt, const dit_kv_cache* cache, const int32_t* runs, int n_runs, void* ws,
+                              size_t ws_bytes, hipStream_t stream) {
+  g_last_error.clear();
+  DIT_TRY(check_model_cfg(cfg));
+  DIT_TRY(check_varlen(vl, true));
+  DIT_TRY(check_text_weights(cfg, w));
+  DIT_TRY(check_model_cache(cfg, cache, 0));
+  DIT_TRY(check_ptr(txt, "txt"));
+  if (n_runs < 0 || (int64_t)n_runs * 2 * cache->n_kv_heads > 0x7FFFFFFF) return fail(DIT_ERR_INVALID_ARG, "slot map of %d entries", n_runs);
+  DIT_TRY(check_ptr(runs, "runs", n_runs == 0));
+  const size_t need = dit_text_kv_cached_workspace_size(cfg, vl);
+  if (need > 0 && (!ws || ((uintptr_t)ws & 255u))) return fail(DIT_ERR_WORKSPACE, "workspace NULL or not 256-byte aligned (%zu bytes needed)", need);
+  if (ws_bytes < need) return fail(DIT_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
+  const dit_block_config* c = &cfg->block;
+  const int64_t L = vl->cu_seqlens_txt[vl->n_req];
+  if (L == 0) return DIT_OK;
+  const ReqTable req_txt = make_req(vl->cu_seqlens_txt, vl->n_req);
+  const int D = c->hidden;
+  for (int b = 0; b < cfg->n_blocks; ++b) {
+    DIT_TRY(text_kv_impl(c, &w->blocks[b], L, req_txt, txt, ws, stream));
+    DIT_TRY(run_cache_store(cache, b, ws, (char*)ws + D * elem_size(c->dtype), 2 * D, 2 * D, L, runs, n_runs, c->dtype, stream));
+  }
+  return DIT_OK;
+}
+
+size_t dit_denoise_cached_workspace_size(const dit_model_config* cfg, const dit_varlen* vl, const dit_kv_cache* cache) {
+  LatentTable tab;
+  if (check_model_cfg(cfg) != DIT_OK || check_model_varlen(cfg, vl, &tab, false) != DIT_OK ||
+      check_model_cache(cfg, cache, vl->n_req) != DIT_OK)
+    return 0;
+  return model_layout(cfg, vl, nullptr, nullptr) + cached_step_ws(cfg, vl, cache);
+}
+
+dit_status dit_denoise_step_cached(const dit_model_config* cfg, const dit_model_weights* w, const dit_varlen* vl,
+                                   const float* latent, const float* t, const float* dt, const dit_kv_cache* cache,
+                                   float* latent_out, void* ws, size_t ws_bytes, hipStream_t stream) {
+  g_last_error.clear();
+  if (!cache) return fail(DIT_ERR_INVALID_ARG, "cache is NULL");
+  return denoise_step_impl(cfg, w, vl, latent, t, dt, nullptr, cache, latent_out, ws, ws_bytes, stream);
 }
 
 dit_status dit_patchify(const dit_model_config* cfg, const dit_varlen* vl, const float* latent, void* tokens,

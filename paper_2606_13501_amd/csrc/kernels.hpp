@@ -129,4 +129,51 @@ struct LatentArgs {
 hipError_t launch_patchify(const LatentArgs& p, hipStream_t s);
 hipError_t launch_unpatchify_euler(const LatentArgs& p, hipStream_t s);
 
+// ------------------------------------------- the paged 8-bit key/value cache
+
+// Scale bytes that the writer of the pages gives: a code times its scale stays
+// in the normal range of bf16 (2^-9 * 2^-100), and the largest finite input
+// needs 2^120.
+constexpr int kCacheScaleMin = 27, kCacheScaleMax = 247;
+
+struct CacheTablesArgs {
+  int n_req, page_shift, max_pages, rows_per_req, n_rows, n_free, n_runs;
+  const int32_t *lens_before, *added, *free_pages;
+  int32_t *table, *lens, *runs, *counts;
+};
+hipError_t launch_cache_tables(const CacheTablesArgs& p, hipStream_t s);
+
+struct CacheStoreArgs {
+  const void *k, *v;
+  int64_t k_stride, v_stride;   // elements
+  int64_t n_rows;
+  const int32_t* runs;
+  void *k_pages, *v_pages;      // this block's pools
+  uint8_t *k_scale, *v_scale;
+  int n_pages, n_kv_heads, head_dim, page_tokens;
+  dit_dtype dtype;
+  uint32_t n_items = 0;         // set by the launcher
+};
+hipError_t launch_cache_store(CacheStoreArgs p, int n_runs, hipStream_t s);
+
+struct CachedAttnArgs {
+  const void* q;
+  void* o;
+  int64_t q_stride, o_stride;   // elements
+  ReqTable cq;
+  int n_heads, n_kv_heads, head_dim;
+  const char *k_pages, *v_pages;   // this block's pools
+  const uint8_t *k_scale, *v_scale;
+  const int32_t *table, *lens;
+  int n_pages, page_shift, max_pages;
+  int max_len;                  // bound of the lengths: at most max_pages << page_shift
+  float scale;
+  dit_dtype dtype;
+  const void* q_gain = nullptr; // as in AttnArgs
+  float q_eps = 0.f;
+};
+// Bytes of workspace that a launch needs (0: none); only the sizes are read.
+size_t cached_attention_ws(const CachedAttnArgs& p);
+hipError_t launch_cached_attention(const CachedAttnArgs& p, void* ws, hipStream_t s);
+
 }  // namespace dit
