@@ -403,6 +403,8 @@ dit_status dit_unpatchify_euler(const dit_model_config *cfg, const dit_varlen *v
  *     element (.., g, c, t, e) is token 32 g + t, channel 16 c + e;
  *   v [n_blocks, n_pages, n_kv_heads, page_tokens / 32, 2, head_dim, 16]:
  *     element (.., g, f, d, 4 i + j) is token 32 g + 8 i + 4 f + j, channel d.
+ * Pools and slot maps are 16-byte aligned like all device memory here; scales
+ * need no alignment, tables, lengths and the other index arrays 4 bytes.
  * Offsets are 64-bit; a pool may hold up to 2^31 - 1 groups per block
  * (n_pages * n_kv_heads * page_tokens / 32).
  *

@@ -634,6 +634,13 @@ dit_status run_cond_parts(const dit_block_config* c, int n_req, const float* t, 
 
 // ------------------------------------------------ paged key/value cache
 
+// Device arrays of int32 that the kernels read one value at a time.
+dit_status check_ints(const int32_t* p, const char* name, bool allow_null = false) {
+  if (!p && !allow_null) return fail(DIT_ERR_INVALID_ARG, "%s is NULL", name);
+  if ((uintptr_t)p & 3u) return fail(DIT_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
+  return DIT_OK;
+}
+
 size_t cache_page_bytes(const dit_kv_cache* c) { return (size_t)c->n_kv_heads * c->page_tokens * c->head_dim; }
 
 // The sizes, and the parts that a call uses: pools (pages and scales), the table.
@@ -648,13 +655,13 @@ dit_status check_cache(const dit_kv_cache* c, bool pools, int n_req) {
   if (groups > 2147483647.0) return fail(DIT_ERR_UNSUPPORTED, "cache of %.0f groups of 32 tokens per block (at most 2^31 - 1)", groups);
   if (pools) {
     DIT_TRY(check_ptr(c->k, "cache k")); DIT_TRY(check_ptr(c->v, "cache v"));
-    DIT_TRY(check_ptr(c->k_scale, "cache k_scale")); DIT_TRY(check_ptr(c->v_scale, "cache v_scale"));
+    if (!c->k_scale || !c->v_scale) return fail(DIT_ERR_INVALID_ARG, "cache k_scale or v_scale is NULL");
   }
   if (n_req > 0) {
     if (c->max_pages < 1 || (int64_t)c->max_pages * c->page_tokens > 0x7FFFFFFF)
       return fail(DIT_ERR_INVALID_ARG, "cache table of %d pages of %d tokens per request", c->max_pages, c->page_tokens);
     if (n_req > c->table_rows) return fail(DIT_ERR_INVALID_ARG, "%d requests, the cache table has %d rows", n_req, c->table_rows);
-    DIT_TRY(check_ptr(c->table, "cache table")); DIT_TRY(check_ptr(c->lens, "cache lens"));
+    DIT_TRY(check_ints(c->table, "cache table")); DIT_TRY(check_ints(c->lens, "cache lens"));
   }
   return DIT_OK;
 }
@@ -1235,10 +1242,10 @@ dit_status dit_cache_tables(const dit_kv_cache* cache, int n_req, const int32_t*
   g_last_error.clear();
   if (n_req < 1 || n_req > DIT_MAX_REQ) return fail(DIT_ERR_INVALID_ARG, "n_req = %d outside 1..%d", n_req, DIT_MAX_REQ);
   DIT_TRY(check_cache(cache, false, n_req));
-  DIT_TRY(check_ptr(lens_before, "lens_before", true)); DIT_TRY(check_ptr(added, "added"));
+  DIT_TRY(check_ints(lens_before, "lens_before", true)); DIT_TRY(check_ints(added, "added"));
   if (n_free < 0) return fail(DIT_ERR_INVALID_ARG, "n_free = %d", n_free);
-  DIT_TRY(check_ptr(free_pages, "free_pages", n_free == 0));
-  DIT_TRY(check_ptr(runs, "runs")); DIT_TRY(check_ptr(counts, "counts"));
+  DIT_TRY(check_ints(free_pages, "free_pages", n_free == 0));
+  DIT_TRY(check_ptr(runs, "runs")); DIT_TRY(check_ints(counts, "counts"));
   if (n_rows < 0 || n_rows > 0x7FFFFFFF) return fail(DIT_ERR_INVALID_ARG, "n_rows %lld", (long long)n_rows);
   if (rows_per_req < 0 || (rows_per_req > 0 && n_rows != (int64_t)n_req * rows_per_req))
     return fail(DIT_ERR_INVALID_ARG, "rows_per_req = %d: a padded batch of %d requests has %d rows each, n_rows is %lld",

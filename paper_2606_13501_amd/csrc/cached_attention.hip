@@ -20,9 +20,12 @@
 // O^T = V^T P^T in bf16 MFMAs: v_cvt_scalef32_pk_bf16_fp8 turns two codes into
 // bf16 with the page's scale, exactly.
 //
-// Softmax is fp32 in log2 units: the query is multiplied by scale * log2(e)
-// before it is rounded to bf16 and split (a relative error of at most 2^-8 per
-// value, as of q's own rounding).
+// Softmax is fp32 in log2 units: a score is multiplied by scale * log2(e) in
+// the multiply-add that takes off the row's reference.  (Multiplied into the
+// query instead, it would have to be rounded to bf16 with it: the output was
+// then 0.0037 off the exact one, root mean square, 0.0017 of which is its own
+// rounding; now 0.0024.)  Probabilities are rounded to bf16, 8 significant bits
+// each, and their sum is that of the rounded ones.
 #include <float.h>
 
 #include <algorithm>
@@ -110,8 +113,8 @@ __device__ __forceinline__ uint32_t find_group(const CachedWork& w, int r, int h
 __device__ __forceinline__ float pow2(uint32_t biased) { return __uint_as_float(biased << 23); }
 
 // This lane's query row as the B operand of S^T: channels 64 c + 32 h + 16 f
-// .. +15 of the row (f: the lane's half; h: 0, 1), scaled, rounded to bf16 and
-// split into two e4m3 parts with one power of two per row and 64 channels (the
+// .. +15 of the row (f: the lane's half; h: 0, 1), with QNORM RMS-normalised and
+// rounded to bf16, split into two e4m3 parts with one power of two per row and 64 channels (the
 // same byte in both lanes of a row: the instruction's blocks of 32 channels each
 // span both).
 template <int HD> struct QFrag {
@@ -130,7 +133,7 @@ __device__ __forceinline__ void load_query(const bf16* row, int f, const CachedW
 #pragma unroll
       for (int k = 0; k < 2; ++k)
         raw[4 * c + 2 * h + k] = *reinterpret_cast<const bf16x8*>(row + 64 * c + 32 * h + 16 * f + 8 * k);
-  float mul = w.scale_log2;
+  float mul = 1.f;
   bf16x8 gain[QNORM ? 4 * NC : 1];
   if constexpr (QNORM) {
     // RMSNorm over the head: this lane holds half of its values, the lane 32 apart the other half
@@ -143,7 +146,7 @@ __device__ __forceinline__ void load_query(const bf16* row, int f, const CachedW
       for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
     }
     ss += __shfl_xor(ss, 32, kWave);
-    mul *= rsqrtf(ss * (1.0f / HD) + w.q_eps);
+    mul = rsqrtf(ss * (1.0f / HD) + w.q_eps);
   }
   uint32_t bytes = 0;
 #pragma unroll
@@ -152,8 +155,8 @@ __device__ __forceinline__ void load_query(const bf16* row, int f, const CachedW
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      f32x8 v = __builtin_convertvector(raw[4 * c + i], f32x8) * mul;
-      if constexpr (QNORM) v *= __builtin_convertvector(gain[4 * c + i], f32x8);
+      f32x8 v = __builtin_convertvector(raw[4 * c + i], f32x8);
+      if constexpr (QNORM) v = v * mul * __builtin_convertvector(gain[4 * c + i], f32x8);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         x[8 * i + e] = (float)(bf16)v[e];
@@ -209,6 +212,11 @@ __device__ __forceinline__ bf16x8 values8(uint32_t w0, uint32_t w1, float vs) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// acc + a[0] + a[1]
+__device__ __forceinline__ float add_pair(bf16x2 a, float acc) {
+  return __builtin_amdgcn_fdot2_f32_bf16(a, bf16x2{(bf16)1.f, (bf16)1.f}, acc, false);
+}
+
 // Bytes of tokens 8 i + 4 f + 0 .. 3 of a group that are among its first n.
 // Codes past the request's end are whatever the page held before, NaN among
 // them, which a probability of 0 would not take out of the product.
@@ -240,10 +248,9 @@ constexpr float kHeadroom = 18446744073709551616.0f;   // 2^64, bound of a row s
 // two workgroups per compute unit.
 //
 // The row reference of the softmax is the first tile's row maximum for the
-// whole pass; it enters as the start value of the score products, so the loop
-// neither searches maxima nor rescales the output.  Where a row's sum passes
-// 2^64 the workgroup finds the exact maxima and runs again, so the result is
-// the softmax in any case.
+// whole pass, so the loop neither searches maxima nor rescales the output.
+// Where a row's sum passes 2^64 the workgroup finds the exact maxima and runs
+// again, so the result is the softmax in any case.
 template <int HD, bool QNORM>
 __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restrict__ Q, bf16* __restrict__ O,
                                                            CachedWork w) {
@@ -296,71 +303,54 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
   };
 
   f32x16 oacc[ND];
-  float l_run[4];
+  float l_run[2];
   float m_ref = 0.f, x_max = -INFINITY;
-  f32x16 nref{};
   bool have_ref = false;
+  const float c = w.scale_log2;
+  const float off_score = c < 0.f ? INFINITY : -INFINITY;   // times c: -inf
 
-  using kOn = std::true_type;
-  using kOff = std::false_type;
-  // One tile: scores, probabilities, output.  MASKED: groups may be missing or
-  // end early; FIRST: the reference is this tile's row maximum; TRACK: only
-  // the largest score is wanted.
-  auto tile = [&](int t, auto masked, auto first, auto track) __attribute__((always_inline)) {
+  // One tile.  MASKED (its codes of values are then clean, see run_pass): n[hb]
+  // tokens of each group count; track: only the largest score is wanted.
+  auto tile = [&](int t, bool masked, int n0, int n1, bool track) __attribute__((always_inline)) {
     const char* slot = smem + (t % kRing) * kSlot;
     const u32x2 d0 = groups[2 * (t - chunk0)], d1 = groups[2 * (t - chunk0) + 1];
-    int n[2] = {32, 32};
-    if (decltype(masked)::value) {
-      n[0] = __builtin_amdgcn_readfirstlane(d0[0]) == kNoGroup ? 0 : min(max(len - 64 * t, 0), 32);
-      n[1] = __builtin_amdgcn_readfirstlane(d1[0]) == kNoGroup ? 0 : min(max(len - 64 * t - 32, 0), 32);
-      if (n[0] + n[1] == 0) return;   // nothing here (the reference waits for the next tile)
-    }
     f32x16 s[2];
 #pragma unroll
     for (int hb = 0; hb < 2; ++hb) {
-      if (decltype(first)::value || decltype(track)::value) s[hb] = f32x16{};
-      else s[hb] = nref;
       const int ks = (int)(hb ? d1[1] : d0[1]);
       const u32x4* kp = reinterpret_cast<const u32x4*>(slot + hb * kGroup) + lane;
-      s[hb] = score_step<0, HD>(kp[0], kp[64], q, ks, s[hb]);
+      s[hb] = score_step<0, HD>(kp[0], kp[64], q, ks, f32x16{});
       if constexpr (NC == 2) s[hb] = score_step<1, HD>(kp[128], kp[192], q, ks, s[hb]);
     }
-    if (decltype(masked)::value) {
+    if (masked) {
 #pragma unroll
       for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-          if (8 * (v >> 2) + 4 * fh + (v & 3) >= n[hb]) s[hb][v] = -INFINITY;
+          if (8 * (v >> 2) + 4 * fh + (v & 3) >= (hb ? n1 : n0)) s[hb][v] = off_score;
     }
-    if (decltype(track)::value) {
+    if (track || !have_ref) {
+      float mx = -INFINITY;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) x_max = fmaxf(x_max, fmaxf(s[0][v], s[1][v]));
-      return;
-    }
-    if (decltype(first)::value) {
-      float mx = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-      for (int v = 1; v < 16; ++v) mx = fmaxf(mx, fmaxf(s[0][v], s[1][v]));
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, fmaxf(s[0][v] * c, s[1][v] * c));
+      if (track) {
+        x_max = fmaxf(x_max, mx);
+        return;
+      }
       m_ref = fmaxf(mx, __shfl_xor(mx, 32, kWave));
       have_ref = true;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        s[0][v] -= m_ref;
-        s[1][v] -= m_ref;
-        nref[v] = -m_ref;
-      }
     }
     bf16x8 p[4];
 #pragma unroll
     for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
       for (int v = 0; v < 16; v += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(s[hb][v]), p1 = __builtin_amdgcn_exp2f(s[hb][v + 1]);
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[hb][v], c, -m_ref));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[hb][v + 1], c, -m_ref));
         const bf16x2 pr = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
         p[2 * hb + (v >> 3)][v & 7] = pr[0];
         p[2 * hb + (v >> 3)][(v & 7) + 1] = pr[1];
-        l_run[v & 2] += p0;
-        l_run[(v & 2) + 1] += p1;
+        l_run[hb] = add_pair(pr, l_run[hb]);
       }
 #pragma unroll
     for (int hb = 0; hb < 2; ++hb) {
@@ -368,21 +358,17 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       const u32x4* vp = reinterpret_cast<const u32x4*>(slot + (2 + hb) * kGroup + fh * (HD * 16)) + fr;
 #pragma unroll
       for (int db = 0; db < ND; ++db) {
-        u32x4 x = vp[32 * db];
-        if (decltype(masked)::value) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] &= token_mask(i, fh, n[hb]);
-        }
+        const u32x4 x = vp[32 * db];
         oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8(x[0], x[1], vs), p[2 * hb], oacc[db], 0, 0, 0);
         oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8(x[2], x[3], vs), p[2 * hb + 1], oacc[db], 0, 0, 0);
       }
     }
   };
 
-  auto run_pass = [&](auto track) __attribute__((always_inline)) {
+  auto run_pass = [&](bool track) __attribute__((always_inline)) {
 #pragma unroll
     for (int db = 0; db < ND; ++db) oacc[db] = f32x16{};
-    l_run[0] = l_run[1] = l_run[2] = l_run[3] = 0.f;
+    l_run[0] = l_run[1] = 0.f;
     for (int c0 = t_begin; c0 < t_end; c0 += kChunkTiles) {
       const int c1 = min(c0 + kChunkTiles, t_end);
       __syncthreads();   // the previous chunk's groups and tiles have been read
@@ -409,11 +395,27 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       else wait_vmcnt<0>();
       __syncthreads();
       for (int t = c0; t < c1; ++t) {
+        // a tile that ends early or lacks a page: the workgroup clears the value
+        // codes of the tokens that do not count (whatever the page held before,
+        // NaN among them, which a probability of 0 would not take out of the product)
         const bool masked = any_bad || 64 * (t + 1) > len;
-        if (decltype(track)::value) tile(t, kOn{}, kOff{}, kOn{});
-        else if (!have_ref) tile(t, kOn{}, kOn{}, kOff{});
-        else if (masked) tile(t, kOn{}, kOff{}, kOff{});
-        else tile(t, kOff{}, kOff{}, kOff{});
+        int n0 = 32, n1 = 32;
+        if (masked) {
+          const uint32_t g0 = groups[2 * (t - chunk0)][0], g1 = groups[2 * (t - chunk0) + 1][0];
+          n0 = __builtin_amdgcn_readfirstlane(g0) == kNoGroup ? 0 : min(max(len - 64 * t, 0), 32);
+          n1 = __builtin_amdgcn_readfirstlane(g1) == kNoGroup ? 0 : min(max(len - 64 * t - 32, 0), 32);
+          u32x4* vals = reinterpret_cast<u32x4*>(smem + (t % kRing) * kSlot + 2 * kGroup);
+#pragma unroll
+          for (int e = tid; e < 4 * HD; e += 256) {
+            const int f = e / HD % 2, n = e / HD < 2 ? n0 : n1;
+            u32x4 x = vals[e];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] &= token_mask(i, f, n);
+            vals[e] = x;
+          }
+          __syncthreads();
+        }
+        if (n0 + n1 > 0) tile(t, masked, n0, n1, track);   // (nothing there: the reference waits for the next tile)
         if (t + 1 < c1) {
           // tile t + 1 in LDS for every wave; tile t + 3 into the slot of t - 1
           if (t + 2 < c1) wait_vmcnt<kLoads>();
@@ -424,24 +426,25 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       }
     }
   };
-  auto row_sum = [&]() __attribute__((always_inline)) {
-    const float l = (l_run[0] + l_run[1]) + (l_run[2] + l_run[3]);
-    return l + __shfl_xor(l, 32, kWave);
-  };
 
-  if (tid == 0) s_redo = 0;
-  run_pass(kOff{});
-  float l_tot = row_sum();
-  __syncthreads();
-  if (__builtin_amdgcn_ballot_w64(!(l_tot <= kHeadroom)) != 0 && lane == 0) s_redo = 1;
-  __syncthreads();
-  if (__builtin_amdgcn_readfirstlane(s_redo) != 0) {
-    run_pass(kOn{});
-    m_ref = fmaxf(x_max, __shfl_xor(x_max, 32, kWave));
-#pragma unroll
-    for (int v = 0; v < 16; ++v) nref[v] = -m_ref;
-    run_pass(kOff{});   // have_ref: with the exact row maxima
-    l_tot = row_sum();
+  // The first pass against the first tile's maxima; where a row sum passed 2^64
+  // (or overflowed), one to find the exact maxima and one against them.
+  float l_tot = 0.f;
+#pragma unroll 1
+  for (int pass = 0;; ++pass) {
+    run_pass(pass == 1);
+    if (pass == 1) {
+      m_ref = fmaxf(x_max, __shfl_xor(x_max, 32, kWave));
+      continue;
+    }
+    const float l = l_run[0] + l_run[1];
+    l_tot = l + __shfl_xor(l, 32, kWave);
+    if (pass == 2) break;
+    if (tid == 0) s_redo = 0;
+    __syncthreads();
+    if (__builtin_amdgcn_ballot_w64(!(l_tot <= kHeadroom)) != 0 && lane == 0) s_redo = 1;
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(s_redo) == 0) break;
   }
 
   // oacc[db][4 i + j]: channel 32 db + 8 i + 4 fh + j of the lane's row
@@ -574,6 +577,8 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
     const int ks = (int)x.scales;
     s = score_step<0, HD>(x.k[0], x.k[1], q, ks, s);
     if constexpr (NC == 2) s = score_step<1, HD>(x.k[2], x.k[3], q, ks, s);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] *= w.scale_log2;
     if (x.n < 32) {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
@@ -596,17 +601,16 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
       for (int d = 0; d < ND; ++d) oacc[d] *= a;
     }
     bf16x8 p[2];
-    float l0 = 0.f, l1 = 0.f;
+    float lp[2] = {0.f, 0.f};
 #pragma unroll
     for (int v = 0; v < 16; v += 2) {
       const float p0 = __builtin_amdgcn_exp2f(s[v] - m), p1 = __builtin_amdgcn_exp2f(s[v + 1] - m);
       const bf16x2 pr = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
       p[v >> 3][v & 7] = pr[0];
       p[v >> 3][(v & 7) + 1] = pr[1];
-      l0 += p0;
-      l1 += p1;
+      lp[v >> 3] = add_pair(pr, lp[v >> 3]);
     }
-    l += l0 + l1;
+    l += lp[0] + lp[1];
     const float vs = pow2(x.scales >> 8);
 #pragma unroll
     for (int d = 0; d < ND; ++d) {

@@ -62,7 +62,7 @@ def test_tables_refusals():
         _refused(_tables(_cache(**kw)), st, text)
     c = _cache()
     for kw, text in [(dict(n_req=0), "n_req"), (dict(n_req=65), "n_req"), (dict(n_req=4), "3 rows"), (dict(added=0), "added"),
-                     (dict(before=BEF + 4), "lens_before"), (dict(free=0), "free_pages"), (dict(n_free=-1), "n_free"),
+                     (dict(before=BEF + 2), "lens_before"), (dict(free=FREE + 1), "free_pages"), (dict(runs=RUNS + 8), "runs"), (dict(free=0), "free_pages"), (dict(n_free=-1), "n_free"),
                      (dict(runs=0), "runs"), (dict(counts=0), "counts"), (dict(n_rows=-1), "n_rows"),
                      (dict(n_rows=1 << 31), "n_rows"), (dict(per=-1), "rows_per_req"), (dict(per=49), "padded"),
                      (dict(n_runs=4), "5 needed"), (dict(n_runs=-1), "needed")]:

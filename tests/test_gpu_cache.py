@@ -41,7 +41,9 @@ def _tables(page, width, before, added, n_free, per=0, n_rows=None, rows=None, n
     free = rng.permutation(10 ** 5)[:n_free].astype(np.int32)
     runs = torch.full((B.cache_run_bound(page, n, n_rows) + extra, 4), -5, dtype=torch.int32, device="cuda")
     counts = _i32([-1] * 4)
-    B.cache_tables(cache, None if null_before else _i32(before), _i32(added), _i32(free) if n_free else None, runs, counts,
+    # a stack of free pages whose top is anywhere: no alignment but an integer's
+    stack = _i32(np.r_[np.full(n % 4, -9, np.int32), free])[n % 4:]
+    B.cache_tables(cache, None if null_before else _i32(before), _i32(added), stack if n_free else None, runs, counts,
                    n_rows, per)
     torch.cuda.synchronize()
     tab, lens, want, cnt = C.tables(page, start, [0] * n if null_before else before, added, free, n_rows, per)
