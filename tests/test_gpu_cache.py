@@ -333,7 +333,7 @@ def test_attention_long_history(qlens):
     """Past the groups that are looked up at once (32,768 tokens), divided or not."""
     B, cache, q, cu, H = _case(BF16, 128, 64, 1, 1, qlens, [70001], seed=12)
     _check_attention(cache, q, _attend(B, cache, q, cu, H), cu, H, rows=12)
-    many = torch.cat([q] * (-(-128 * 512 // len(q))))[:128 * 512].contiguous()   # as many tiles as run at once: one piece
+    many = torch.cat([q] * (-(-128 * 2048 // len(q))))[:128 * 2048].contiguous()   # four rounds of workgroups: not divided
     cu = [0, len(many)]
     assert B.attention_cached_workspace_size(cache, cu, H, BF16) == 0
     _check_attention(cache, many, _attend(B, cache, many, cu, H), cu, H, rows=12)
