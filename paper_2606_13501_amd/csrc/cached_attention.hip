@@ -690,10 +690,8 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
     const int g_begin = 4 * it.u0, g_end = min(4 * it.u1, (len + 31) / 32);   // units of 128 tokens
     const int n_mine = max(0, (g_end - g_begin - wave + WAVES - 1) / WAVES);   // groups g_begin + wave + 4 i
 
-    QFrag<HD> q;
     bf16x8 raw[HD / 16];
     load_row<HD>(Q + (int64_t)token * w.q_stride + (it.head * w.group + row % w.group) * HD, fh, raw);
-    split_row<HD, QNORM>(raw, fh, w, q);
 
     uint32_t at = kNoGroup, scales = 0;   // lane i: this wave's group base + i
     int base = 0;
@@ -704,13 +702,9 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
     };
     struct Group {
       u32x4 k[2 * NC], v[ND];
-      int n;             // its valid tokens
-      uint32_t scales;
     };
     auto fetch = [&](int i, Group& x) __attribute__((always_inline)) {
       const uint32_t g = __builtin_amdgcn_readlane(at, i - base);
-      x.scales = __builtin_amdgcn_readlane(scales, i - base);
-      x.n = g == kNoGroup ? 0 : min(len - 32 * (g_begin + wave + WAVES * i), 32);
       // a group that is not there: the pool's first is loaded and not used
       const uint64_t off = (uint64_t)(g == kNoGroup ? 0u : g) * kGroup;
       const u32x4* kp = reinterpret_cast<const u32x4*>(w.k_pages + off) + lane;
@@ -725,22 +719,26 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
 #pragma unroll
     for (int d = 0; d < ND; ++d) oacc[d] = f32x16{};
     float m = -INFINITY, l = 0.f;
-    auto compute = [&](Group& x) __attribute__((always_inline)) {
-      if (x.n == 0) return;
+    QFrag<HD> q;
+    auto compute = [&](int i, Group& x) __attribute__((always_inline)) {
+      const bool there = __builtin_amdgcn_readlane(at, i - base) != kNoGroup;
+      const uint32_t sc = __builtin_amdgcn_readlane(scales, i - base);
+      const int n = there ? min(len - 32 * (g_begin + wave + WAVES * i), 32) : 0;   // its valid tokens
+      if (n == 0) return;
       f32x16 s{};
-      const int ks = (int)x.scales;
+      const int ks = (int)sc;
       s = score_step<0, HD>(x.k[0], x.k[1], q, ks, s);
       if constexpr (NC == 2) s = score_step<1, HD>(x.k[2], x.k[3], q, ks, s);
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] *= w.scale_log2;
-      if (x.n < 32) {
+      if (n < 32) {
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-          if (8 * (v >> 2) + 4 * fh + (v & 3) >= x.n) s[v] = -INFINITY;
+          if (8 * (v >> 2) + 4 * fh + (v & 3) >= n) s[v] = -INFINITY;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x.v[d][i] &= token_mask(i, fh, x.n);
+          for (int i = 0; i < 4; ++i) x.v[d][i] &= token_mask(i, fh, n);
       }
       float mx = s[0];
 #pragma unroll
@@ -766,7 +764,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
         lp[1] += p1;
       }
       l += lp[0] + lp[1];
-      const float vs = pow2(x.scales >> 8);
+      const float vs = pow2(sc >> 8);
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
         oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values8(x.v[d][0], x.v[d][1], vs), p[0], oacc[d], 0, 0, 0);
@@ -774,16 +772,24 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
       }
     };
 
+    // the first tokens are on their way before the queries are split
+    Group a, b;
+    if (n_mine > 0) {
+      look_up(0);
+      fetch(0, a);
+    }
+    split_row<HD, QNORM>(raw, fh, w, q);
     for (int i0 = 0; i0 < n_mine; i0 += kWave) {
-      look_up(i0);
+      if (i0 > 0) {
+        look_up(i0);
+        fetch(i0, a);
+      }
       const int n = min(n_mine - i0, kWave);
-      Group a, b;
-      fetch(i0, a);
       for (int i = 0; i < n; i += 2) {
         if (i + 1 < n) fetch(i0 + i + 1, b);
-        compute(a);
+        compute(i0 + i, a);
         if (i + 2 < n) fetch(i0 + i + 2, a);
-        if (i + 1 < n) compute(b);
+        if (i + 1 < n) compute(i0 + i + 1, b);
       }
     }
     l += __shfl_xor(l, 32, kWave);
@@ -942,18 +948,27 @@ __global__ __launch_bounds__(256) void cached_attn_merge(T* __restrict__ O, Cach
     if (s0 == s1) return;   // written by its workgroup
     const f32x2* ml = reinterpret_cast<const f32x2*>(w.part + (int64_t)2 * w.shares * w.tile_rows * HD);
     const int at = row - tile * w.tile_rows;
+    // four parts' loads at a time, joined in order
     float top = -INFINITY, l = 0.f;
-    for (int s = s0; s <= s1; ++s) {
-      const f32x2 x = ml[(int64_t)(2 * s + (s == s0)) * w.tile_rows + at];
-      if (x[1] != 0.f) top = fmaxf(top, x[0]);
-    }
-    for (int s = s0; s <= s1; ++s) {
-      const int64_t slot_row = (int64_t)(2 * s + (s == s0)) * w.tile_rows + at;
-      const f32x2 x = ml[slot_row];
-      if (x[1] == 0.f) continue;   // no keys
-      const float a = exp2f(x[0] - top);
-      l = fmaf(a, x[1], l);
-      o += *reinterpret_cast<const f32x4*>(w.part + slot_row * HD + d) * a;
+    for (int s = s0; s <= s1; s += 4) {
+      f32x2 x[4];
+      f32x4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int at_s = min(s + k, s1);
+        const int64_t slot_row = (int64_t)(2 * at_s + (at_s == s0)) * w.tile_rows + at;
+        x[k] = ml[slot_row];
+        v[k] = *reinterpret_cast<const f32x4*>(w.part + slot_row * HD + d);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (s + k > s1 || x[k][1] == 0.f) continue;   // no such part, or one without keys
+        const float m = fmaxf(top, x[k][0]);
+        const float a = exp2f(top - m), b = exp2f(x[k][0] - m);   // (the first: 2^-inf = 0)
+        l = fmaf(b, x[k][1], l * a);
+        o = o * a + v[k] * b;
+        top = m;
+      }
     }
     o *= l != 0.f ? 1.0f / l : 0.f;
   }
