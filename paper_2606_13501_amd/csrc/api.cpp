@@ -710,13 +710,13 @@ CachedAttnArgs cached_args(const dit_kv_cache* c, int block, const void* q, void
   return p;
 }
 
-// Work items (128 query rows of a key/value head or fewer, up to 64 key pieces
-// each) are numbered in 23 bits: a launch of fewer than 2^32 work-items.
+// Workgroups (128 query rows of a key/value head each, or fewer) are numbered
+// in 22 bits: a launch of fewer than 2^32 work-items.
 dit_status check_cached_items(const dit_kv_cache* c, const int32_t* cu, int n_req, int n_heads, dit_dtype dt) {
   const int64_t group = n_heads / c->n_kv_heads, rows = dt == DIT_F32 ? 16 : 128;
   int64_t items = 0;
   for (int r = 0; r < n_req; ++r) items += ((cu[r + 1] - cu[r]) * group + rows - 1) / rows * c->n_kv_heads;
-  if (items > (1 << 23)) return fail(DIT_ERR_UNSUPPORTED, "cached attention of %lld work items (at most 2^23)", (long long)items);
+  if (items > (1 << 22)) return fail(DIT_ERR_UNSUPPORTED, "cached attention of %lld work items (at most 2^22)", (long long)items);
   return DIT_OK;
 }
 

@@ -186,6 +186,25 @@ __device__ __forceinline__ uint32_t find_group(const CachedWork& w, int r, int h
   return (slot << gs) + (g & ((1 << gs) - 1));
 }
 
+// Sum and maximum of a lane's value and that of the lane 32 (or 16) apart.
+template <int N> __device__ __forceinline__ u32x2 swap_lanes(uint32_t x) {
+  if constexpr (N == 32) {
+    const auto sw = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return u32x2{sw[0], sw[1]};
+  } else {
+    const auto sw = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return u32x2{sw[0], sw[1]};
+  }
+}
+template <int N> __device__ __forceinline__ float pair_max(float x) {
+  const u32x2 sw = swap_lanes<N>(__float_as_uint(x));
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+template <int N> __device__ __forceinline__ float pair_sum(float x) {
+  const u32x2 sw = swap_lanes<N>(__float_as_uint(x));
+  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
+
 __device__ __forceinline__ float pow2(uint32_t biased) { return __uint_as_float(biased << 23); }
 
 // This lane's query row as the B operand of S^T: channels 64 c + 32 h + 16 f
@@ -220,7 +239,7 @@ __device__ __forceinline__ void split_row(const bf16x8 (&raw)[HD / 16], int f, c
 #pragma unroll
       for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
     }
-    ss += __shfl_xor(ss, 32, kWave);
+    ss = pair_sum<32>(ss);
     mul = rsqrtf(ss * (1.0f / HD) + w.q_eps);
   }
   uint32_t bytes = 0;
@@ -238,7 +257,8 @@ __device__ __forceinline__ void split_row(const bf16x8 (&raw)[HD / 16], int f, c
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = max(top, max(bits[e] << 16 & 0x7FFF0000u, bits[e] & 0x7FFF0000u));
     }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32, kWave));
+    const u32x2 both = swap_lanes<32>(top);
+    top = max(both[0], both[1]);
     // smallest power of two with every value of the row's 64 channels (this
     // lane's and the lane's 32 apart) at most 448 = 1.75 * 2^8 of it; 16 and more,
     // so that the low part's byte stays positive.  A row with an infinity or NaN
@@ -547,7 +567,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
 #pragma unroll
                 for (int v = 0; v < 16; ++v) mx = fmaxf(mx, fmaxf(s[0][v] * c, s[1][v] * c));
                 if (track) x_max = fmaxf(x_max, mx);
-                else m_ref = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+                else m_ref = pair_max<32>(mx);
                 have_ref = true;
               }
               if (!track) output(t, s);
@@ -566,11 +586,10 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
     for (int pass = 0;; ++pass) {
       run_pass(pass == 1);
       if (pass == 1) {
-        m_ref = fmaxf(x_max, __shfl_xor(x_max, 32, kWave));
+        m_ref = pair_max<32>(x_max);
         continue;
       }
-      const float l = l_run[0] + l_run[1];
-      l_tot = l + __shfl_xor(l, 32, kWave);
+      l_tot = pair_sum<32>(l_run[0] + l_run[1]);
       if (tid == 0) s_redo = 0;
       __syncthreads();   // (and every wave has read its last tile: the ring is free)
       if (pass == 2) break;
@@ -623,11 +642,11 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
 
 // ------------------------------------------------ the waves' shares, joined
 
-// Row `row` of a workgroup's tile: WAVES partial outputs o[wave][channel][row],
+// Row `row` of a workgroup's tile: WAVES partial outputs o[wave][row][channel],
 // references m and sums l (log2 units; l 0: no keys), joined in wave order, then
 // written to the output or, unfinished, to the segment's slot.
 template <int HD, int ROWS, int WAVES, typename T>
-__device__ __forceinline__ void join_waves(const float (&o)[WAVES][HD][ROWS + 1], const float (&m)[WAVES][ROWS],
+__device__ __forceinline__ void join_waves(const float (&o)[WAVES][ROWS][HD + 4], const float (&m)[WAVES][ROWS],
                                            const float (&l)[WAVES][ROWS], int row0, int rows, const Segment& it,
                                            const CachedWork& w, T* O) {
   for (int e = threadIdx.x; e < min(ROWS, rows - row0) * HD; e += WAVES * kWave) {
@@ -645,7 +664,7 @@ __device__ __forceinline__ void join_waves(const float (&o)[WAVES][HD][ROWS + 1]
       if (l[v][i] != 0.f) {
         const float a = exp2f(m[v][i] - top);
         sum = fmaf(a, l[v][i], sum);
-        acc = fmaf(a, o[v][d][i], acc);
+        acc = fmaf(a, o[v][i][d], acc);
       }
     if (it.slot >= 0) {
       const int64_t at = (int64_t)it.slot * ROWS + i;
@@ -659,15 +678,18 @@ __device__ __forceinline__ void join_waves(const float (&o)[WAVES][HD][ROWS + 1]
 
 // -------------------------------------------------- bf16, few rows of a head
 
+constexpr int kKeyWaves = 8;   // waves of a workgroup whose waves share the tokens
+
 // At most 32 rows per head: the cache is read once and bounds the time, so the
-// waves share the tokens, not the rows.  Each wave takes every 4th group of 32
+// waves share the tokens, not the rows.  Each wave takes every 8th group of 32
 // tokens of its segment, straight from global memory into registers in the
 // operands' order (whole KiB per load), two groups ahead, with an exact online
 // softmax; the waves meet in LDS, the shares in cached_attn_merge.
 template <int HD, bool QNORM, bool SHARES>
-__global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict__ Q, bf16* __restrict__ O, CachedWork w) {
-  constexpr int NC = HD / 64, ND = HD / 32, kGroup = 32 * HD, WAVES = 4;
-  __shared__ float part_o[WAVES][HD][33];
+__global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __restrict__ Q, bf16* __restrict__ O,
+                                                                  CachedWork w) {
+  constexpr int NC = HD / 64, ND = HD / 32, kGroup = 32 * HD, WAVES = kKeyWaves;
+  __shared__ __attribute__((aligned(16))) float part_o[WAVES][32][HD + 4];
   __shared__ float part_m[WAVES][32], part_l[WAVES][32];
   __shared__ int64_t ends[SHARES ? kWave : 1];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -688,7 +710,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
     const int token = w.q_start[it.i] + row / w.group;
     const int len = __builtin_amdgcn_readfirstlane(length_of(w, r));
     const int g_begin = 4 * it.u0, g_end = min(4 * it.u1, (len + 31) / 32);   // units of 128 tokens
-    const int n_mine = max(0, (g_end - g_begin - wave + WAVES - 1) / WAVES);   // groups g_begin + wave + 4 i
+    const int n_mine = max(0, (g_end - g_begin - wave + WAVES - 1) / WAVES);   // groups g_begin + wave + WAVES i
 
     bf16x8 raw[HD / 16];
     load_row<HD>(Q + (int64_t)token * w.q_stride + (it.head * w.group + row % w.group) * HD, fh, raw);
@@ -743,7 +765,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
       float mx = s[0];
 #pragma unroll
       for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      mx = pair_max<32>(mx);
       if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
         const float m_new = fmaxf(m, mx);
         const float a = __builtin_amdgcn_exp2f(m - m_new);   // the first group: 2^-inf = 0
@@ -773,7 +795,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
     };
 
     // the first tokens are on their way before the queries are split
-    Group a, b;
+    Group a{};
     if (n_mine > 0) {
       look_up(0);
       fetch(0, a);
@@ -785,14 +807,15 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
         fetch(i0, a);
       }
       const int n = min(n_mine - i0, kWave);
-      for (int i = 0; i < n; i += 2) {
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {   // one copy of its code: few tokens wait for the instructions
+        Group b = a;
         if (i + 1 < n) fetch(i0 + i + 1, b);
         compute(i0 + i, a);
-        if (i + 2 < n) fetch(i0 + i + 2, a);
-        if (i + 1 < n) compute(i0 + i + 1, b);
+        a = b;
       }
     }
-    l += __shfl_xor(l, 32, kWave);
+    l = pair_sum<32>(l);
     __syncthreads();   // the previous segment's rows have been read
     if (fh == 0) {
       part_m[wave][fr] = m;
@@ -801,7 +824,9 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) part_o[wave][32 * d + 8 * (v >> 2) + 4 * fh + (v & 3)][fr] = oacc[d][v];
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(&part_o[wave][fr][32 * d + 8 * i + 4 * fh]) =
+            f32x4{oacc[d][4 * i], oacc[d][4 * i + 1], oacc[d][4 * i + 2], oacc[d][4 * i + 3]};
     __syncthreads();
     join_waves<HD, 32, WAVES>(part_o, part_m, part_l, 0, rows, it, w, O);
   } while (SHARES && next_segment(w, ends, share, it));
@@ -809,15 +834,17 @@ __global__ __launch_bounds__(256, 2) void cached_attn_few(const bf16* __restrict
 
 // ------------------------------------------------------------------- fp32
 
-// 16 rows per workgroup; the waves share the groups of 32 tokens, each with an
-// exact online softmax, on the fp32 matrix instruction: S^T = K Q^T on 16 keys
-// leaves a lane four keys of one query, which feed O^T = V^T P^T from its
-// registers.  A lane's four codes of an operand are one dword of the page,
-// converted exactly.  Latency-bound at the small configuration's sizes.
+// 16 rows per workgroup; the waves share the tokens in tiles of 16 (wave v has
+// every 8th), each with an exact online softmax, on the fp32 matrix instruction:
+// S^T = K Q^T on 16 keys leaves a lane four keys of one query, which feed O^T =
+// V^T P^T from its registers.  A lane's four codes of an operand are one dword
+// of the page, converted exactly.  Latency-bound at the small configuration's
+// sizes: the next tile is asked for before the last is computed.
 template <int HD, bool SHARES>
-__global__ __launch_bounds__(256) void cached_attn_f32(const float* __restrict__ Q, float* __restrict__ O, CachedWork w) {
-  constexpr int NB = HD / 16, kGroup = 32 * HD, WAVES = 4;
-  __shared__ float part_o[WAVES][HD][17];
+__global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_f32(const float* __restrict__ Q, float* __restrict__ O,
+                                                                  CachedWork w) {
+  constexpr int NB = HD / 16, kGroup = 32 * HD, WAVES = kKeyWaves;
+  __shared__ __attribute__((aligned(16))) float part_o[WAVES][16][HD + 4];
   __shared__ float part_m[WAVES][16], part_l[WAVES][16];
   __shared__ int64_t ends[SHARES ? kWave : 1];
   const int lane = threadIdx.x & 63;
@@ -844,75 +871,95 @@ __global__ __launch_bounds__(256) void cached_attn_f32(const float* __restrict__
       acc[c] = f32x4{};
     }
     const int len = __builtin_amdgcn_readfirstlane(length_of(w, req));
-    const int g_begin = 4 * it.u0, g_end = min(4 * it.u1, (len + 31) / 32);   // units of 128 tokens
+    const int t_begin = 8 * it.u0, t_end = min(8 * it.u1, (len + 15) / 16);   // units of 128 tokens
+    const int n_mine = max(0, (t_end - t_begin - wave + WAVES - 1) / WAVES);   // tiles t_begin + wave + WAVES i
+    uint32_t at = kNoGroup, scales = 0;   // lane i: the group of this wave's tile base + i
+    int base = 0;
+    auto look_up = [&](int i0) __attribute__((always_inline)) {
+      base = i0;
+      at = kNoGroup;
+      if (i0 + lane < n_mine) at = find_group(w, req, it.head, (t_begin + wave + WAVES * (i0 + lane)) / 2, scales);
+    };
+    struct Tile {
+      uint32_t k[NB], v[NB];
+    };
+    auto fetch = [&](int i, Tile& x) __attribute__((always_inline)) {
+      const uint32_t g = __builtin_amdgcn_readlane(at, i - base);
+      const int h = (t_begin + wave + WAVES * i) & 1;   // half of the group
+      // a group that is not there: the pool's first is loaded and not used
+      const uint64_t off = (uint64_t)(g == kNoGroup ? 0u : g) * kGroup;
+      const char* kp = w.k_pages + off + (16 * h + r) * 16 + 4 * g4;
+      // tokens 16 h + 4 g4 + 0 .. 3: slots 4 i + 0 .. 3 of f = g4 % 2, i = 2 h + g4 / 2
+      const char* vp = w.v_pages + off + (g4 & 1) * (HD * 16) + r * 16 + 4 * (2 * h + (g4 >> 1));
+#pragma unroll
+      for (int c = 0; c < NB; ++c) {
+        x.k[c] = *reinterpret_cast<const uint32_t*>(kp + c * 512);
+        x.v[c] = *reinterpret_cast<const uint32_t*>(vp + c * 256);
+      }
+    };
     float m = -INFINITY, l = 0.f;
-    for (int g = g_begin + wave; g < g_end; g += WAVES) {
-      uint32_t scales;
-      const uint32_t at = __builtin_amdgcn_readfirstlane(find_group(w, req, it.head, g, scales));
-      if (at == kNoGroup) continue;
-      const float ks = pow2(scales & 0xFF) * w.scale_log2, vs = pow2(scales >> 8);
-      const char* kp = w.k_pages + (uint64_t)at * kGroup;
-      const char* vp = w.v_pages + (uint64_t)at * kGroup;
+    auto compute = [&](int i, Tile& x) __attribute__((always_inline)) {
+      if (__builtin_amdgcn_readlane(at, i - base) == kNoGroup) return;
+      const uint32_t sc = __builtin_amdgcn_readlane(scales, i - base);
+      const float ks = pow2(sc & 0xFF) * w.scale_log2, vs = pow2(sc >> 8);
+      const int n = len - 16 * (t_begin + wave + WAVES * i);   // keys from here on
+      f32x4 s0{}, s1{};   // two sums: each product has the time of the other's to come out
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int n = len - 32 * g - 16 * h;   // keys from here on
-        if (n <= 0) break;
-        uint32_t kw[NB], vw[NB];
+      for (int c = 0; c < NB; ++c) {
+        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)x.k[c], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)x.k[c], true);
+        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(a[0], q[c][0], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(a[1], q[c][1], s1, 0, 0, 0);
+        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(b[0], q[c][2], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(b[1], q[c][3], s1, 0, 0, 0);
+      }
+      f32x4 s = s0 + s1;
+      float mx = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < NB; ++c) {
-          kw[c] = *reinterpret_cast<const uint32_t*>(kp + c * 512 + (16 * h + r) * 16 + 4 * g4);
-          // tokens 16 h + 4 g4 + 0 .. 3: slots 4 i + 0 .. 3 of f = g4 % 2, i = 2 h + g4 / 2
-          vw[c] = *reinterpret_cast<const uint32_t*>(vp + (g4 & 1) * (HD * 16) + (16 * c + r) * 16 + 4 * (2 * h + (g4 >> 1)));
-          if (n < 16) vw[c] &= token_mask(0, 0, n - 4 * g4);
-        }
-        f32x4 s{};
+      for (int e = 0; e < 4; ++e) {
+        s[e] = 4 * g4 + e < n ? s[e] * ks : -INFINITY;
+        mx = fmaxf(mx, s[e]);
+      }
+      mx = pair_max<32>(pair_max<16>(mx));
+      const float m_new = fmaxf(m, mx);
+      const float ref = m_new == -INFINITY ? 0.f : m_new;   // scores of -inf only so far
+      const float a = exp2f(m - ref);
+      f32x4 p;
 #pragma unroll
-        for (int c = 0; c < NB; ++c) {
-          const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)kw[c], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)kw[c], true);
-          s = __builtin_amdgcn_mfma_f32_16x16x4f32(a[0], q[c][0], s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_16x16x4f32(a[1], q[c][1], s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_16x16x4f32(b[0], q[c][2], s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_16x16x4f32(b[1], q[c][3], s, 0, 0, 0);
-        }
-        float mx = -INFINITY;
+      for (int e = 0; e < 4; ++e) p[e] = exp2f(s[e] - ref);
+      l = l * a + ((p[0] + p[1]) + (p[2] + p[3]));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[e] = 4 * g4 + e < n ? s[e] * ks : -INFINITY;
-          mx = fmaxf(mx, s[e]);
-        }
-        mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-        const float m_new = fmaxf(m, mx);
-        const float ref = m_new == -INFINITY ? 0.f : m_new;   // scores of -inf only so far
-        const float a = exp2f(m - ref);
-        f32x4 p;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = exp2f(s[e] - ref);
-        l = l * a + ((p[0] + p[1]) + (p[2] + p[3]));
-#pragma unroll
-        for (int c = 0; c < NB; ++c) {
-          const f32x2 x = __builtin_amdgcn_cvt_pk_f32_fp8((int)vw[c], false) * vs;
-          const f32x2 y = __builtin_amdgcn_cvt_pk_f32_fp8((int)vw[c], true) * vs;
-          acc[c] *= a;
-          acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[0], p[0], acc[c], 0, 0, 0);
-          acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[1], p[1], acc[c], 0, 0, 0);
-          acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[0], p[2], acc[c], 0, 0, 0);
-          acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[1], p[3], acc[c], 0, 0, 0);
-        }
-        m = m_new;
+      for (int c = 0; c < NB; ++c) {
+        const uint32_t v = n < 16 ? x.v[c] & token_mask(0, 0, n - 4 * g4) : x.v[c];
+        const f32x2 y = __builtin_amdgcn_cvt_pk_f32_fp8((int)v, false) * vs, z = __builtin_amdgcn_cvt_pk_f32_fp8((int)v, true) * vs;
+        acc[c] *= a;
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[0], p[0], acc[c], 0, 0, 0);
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[1], p[1], acc[c], 0, 0, 0);
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(z[0], p[2], acc[c], 0, 0, 0);
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(z[1], p[3], acc[c], 0, 0, 0);
+      }
+      m = m_new;
+    };
+    for (int i0 = 0; i0 < n_mine; i0 += kWave) {
+      look_up(i0);
+      const int n = min(n_mine - i0, kWave);
+      Tile a;
+      fetch(i0, a);
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {
+        Tile b = a;
+        if (i + 1 < n) fetch(i0 + i + 1, b);
+        compute(i0 + i, a);
+        a = b;
       }
     }
-    l += __shfl_xor(l, 16, kWave);
-    l += __shfl_xor(l, 32, kWave);
+    l = pair_sum<32>(pair_sum<16>(l));
     __syncthreads();   // the previous segment's rows have been read
     if (g4 == 0) {
       part_m[wave][r] = m;
       part_l[wave][r] = l;
     }
 #pragma unroll
-    for (int c = 0; c < NB; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) part_o[wave][16 * c + 4 * g4 + e][r] = acc[c][e];
+    for (int c = 0; c < NB; ++c) *reinterpret_cast<f32x4*>(&part_o[wave][r][16 * c + 4 * g4]) = acc[c];
     __syncthreads();
     join_waves<HD, 16, WAVES>(part_o, part_m, part_l, it.tile * 16, rows, it, w, O);
   } while (SHARES && next_segment(w, ends, share, it));
@@ -978,6 +1025,8 @@ __global__ __launch_bounds__(256) void cached_attn_merge(T* __restrict__ O, Cach
 
 // ------------------------------------------------------------------ launch
 
+constexpr int64_t kMaxItems = (1 << 22);   // 512 threads each: a launch of fewer than 2^32 work-items
+
 enum Shape { kMany, kFew, kF32 };
 
 struct CachedPlan {
@@ -1008,7 +1057,7 @@ CachedPlan plan(const CachedAttnArgs& p, int cus) {
   pl.shares = 0;
   const int64_t items = tiles(pl.tile_rows) * p.n_kv_heads;
   // workgroups that run at once, a multiple of the XCDs
-  const int64_t slots = 2 * (int64_t)std::max(cus / kXcds * kXcds, kXcds);
+  const int64_t slots = (pl.shape == kMany ? 2 : 1) * (int64_t)std::max(cus / kXcds * kXcds, kXcds);
   if (p.max_len > 1024 && items > 0 && items < 4 * slots) {
     const int64_t units = items * ((p.max_len + (1 << pl.unit_shift) - 1) >> pl.unit_shift);
     pl.shares = (int)std::min(slots, ((units + pl.min_share - 1) / pl.min_share + kXcds - 1) / kXcds * kXcds);
@@ -1046,7 +1095,7 @@ hipError_t launch_cached_attention(const CachedAttnArgs& p, void* ws, hipStream_
     w.tiles[n] = (int)(((int64_t)len * w.group + pl.tile_rows - 1) / pl.tile_rows);
     w.prefix[n] = (int)items;
     items += (int64_t)w.tiles[n] * p.n_kv_heads;
-    if (items > (1 << 23)) return hipErrorInvalidValue;   // a launch of fewer than 2^32 work-items
+    if (items > kMaxItems) return hipErrorInvalidValue;
     w.prefix[++n] = (int)items;
   }
   w.n_req = n;
@@ -1066,9 +1115,9 @@ hipError_t launch_cached_attention(const CachedAttnArgs& p, void* ws, hipStream_
     constexpr bool SHARES = decltype(shares)::value;
     const bf16* q = (const bf16*)p.q;
     bf16* o = (bf16*)p.o;
-    if (pl.shape == kF32) cached_attn_f32<HD, SHARES><<<grid, 256, 0, s>>>((const float*)p.q, (float*)p.o, w);
-    else if (pl.shape == kFew && p.q_gain) cached_attn_few<HD, true, SHARES><<<grid, 256, 0, s>>>(q, o, w);
-    else if (pl.shape == kFew) cached_attn_few<HD, false, SHARES><<<grid, 256, 0, s>>>(q, o, w);
+    if (pl.shape == kF32) cached_attn_f32<HD, SHARES><<<grid, 64 * kKeyWaves, 0, s>>>((const float*)p.q, (float*)p.o, w);
+    else if (pl.shape == kFew && p.q_gain) cached_attn_few<HD, true, SHARES><<<grid, 64 * kKeyWaves, 0, s>>>(q, o, w);
+    else if (pl.shape == kFew) cached_attn_few<HD, false, SHARES><<<grid, 64 * kKeyWaves, 0, s>>>(q, o, w);
     else if (p.q_gain) cached_attn_many<HD, true, SHARES><<<grid, 256, 0, s>>>(q, o, w);
     else cached_attn_many<HD, false, SHARES><<<grid, 256, 0, s>>>(q, o, w);
     if constexpr (SHARES) {
