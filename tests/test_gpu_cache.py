@@ -319,6 +319,28 @@ def test_attention_head_groups(dtype, dim, kv_heads, group, qlens, klens):
     _check_attention(cache, q, _attend(B, cache, q, cu, H), cu, H)
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("kv_heads,group,qlens,klens", [
+    (40, 1, [1001, 0, 333, 450], [512, 9, 0, 77]), (24, 1, [33, 2000, 1000], [1, 300, 65]), (8, 5, [1500, 31, 300], [18, 512, 129]),
+    (1, 40, [1664, 3], [500, 64])])
+@pytest.mark.parametrize("page", [32, 256])
+def test_attention_many_rows_on_prompts(dim, kv_heads, group, qlens, klens, page):
+    """More than 8 blocks of 32 rows per compute unit on prompts up to 512
+    tokens (that bound given where the table is wider), missing pages, a bound
+    that ends inside a tile, and the same bits from every call."""
+    B, cache, q, cu, H = _case(BF16, dim, page, kv_heads, group, qlens, klens, seed=20, width=4096 // page)
+    rows = 5 if kv_heads * group > 8 else 40
+    first = _attend(B, cache, q, cu, H, max_len=512)
+    _check_attention(cache, q, first, cu, H, max_len=512, rows=rows)
+    for _ in range(3):
+        assert torch.equal(_attend(B, cache, q, cu, H, max_len=512), first)
+    cache.table[1, 0] = -1
+    cache.table[0, (klens[0] - 1) // page] = cache.c.n_pages
+    _check_attention(cache, q, _attend(B, cache, q, cu, H, max_len=512), cu, H, max_len=512, rows=rows)
+    bound = 70   # inside a tile
+    _check_attention(cache, q, _attend(B, cache, q, cu, H, max_len=bound), cu, H, max_len=bound, rows=rows)
+
+
 @pytest.mark.parametrize("dtype,dim", TYPES)
 @pytest.mark.parametrize("qlens,klens", [([1], [9000]), ([3, 1, 2], [5000, 100, 0]), ([200], [9001]), ([130, 20], [4100, 700])])
 def test_attention_divided_tokens(dtype, dim, qlens, klens):
@@ -374,7 +396,7 @@ def test_attention_softmax_scale(dtype, dim, qlens, scale):
 
 
 @pytest.mark.parametrize("dim", [64, 128])
-@pytest.mark.parametrize("qlens", [[20], [300]])
+@pytest.mark.parametrize("qlens", [[20], [300], [33000]])
 @pytest.mark.parametrize("order", ["rising", "falling"])
 def test_attention_far_scores(dim, qlens, order):
     """Scores that rise by hundreds of octaves from tile to tile (past the range
