@@ -162,8 +162,8 @@ def lib() -> ctypes.CDLL:
         "dit_cache_run_bound": (sz, [i32, i32, i64]),
         "dit_cache_tables": (i32, [PK, i32, vp, vp, i32, i64, vp, i32, vp, i32, vp, vp]),
         "dit_cache_store": (i32, [PK, i32, vp, vp, i64, i64, i64, vp, i32, i32, vp]),
-        "dit_attention_cached_workspace_size": (sz, [PK, PI, i32, i32, i32, i32]),
-        "dit_attention_cached": (i32, [PK, i32, vp, vp, i64, i64, PI, i32, i32, i32, f32, i32, vp, sz, vp]),
+        "dit_attention_cached_workspace_size": (sz, [PK, vp, i32, i32, i32, i32]),
+        "dit_attention_cached": (i32, [PK, i32, vp, vp, i64, i64, vp, i32, i32, i32, f32, i32, vp, sz, vp]),
         "dit_text_kv_cached_workspace_size": (sz, [PM, PV]),
         "dit_text_kv_cached": (i32, [PM, PMW, PV, vp, PK, vp, i32, vp, sz, vp]),
         "dit_denoise_cached_workspace_size": (sz, [PM, PV, PK]),
@@ -463,12 +463,35 @@ def unpatchify_euler(cfg: ModelConfig, vl: Varlen, latent, v, dt, latent_out, st
 # ------------------------------------------- the paged 8-bit key/value cache
 
 
+# These calls take microseconds on the GPU, so their checks are kept short:
+# addresses go as numbers, and a cache's reference and widths are made once.
+
+
 def _want(t, name, dtype, shape=None):
     """The tensor's own layout is what the library reads: type and shape exact, dense."""
-    if t.dtype != dtype or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+    if t.dtype != dtype or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ' (not dense)'}, needed: dense "
                          f"{dtype}{'' if shape is None else ' ' + str(tuple(shape))}")
     return t
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _cache_stream(cache, stream, *tensors):
+    """The stream's handle: the cache, the call's tensors and the stream are on the current GPU."""
+    dev = cache.device
+    if dev < 0:
+        raise ValueError("the cache is not on a GPU")
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"the cache is on {cache.k.device}, a tensor of {t.dtype} {tuple(t.shape)} on {t.device}")
+    s = torch.cuda.current_stream() if stream is None else stream
+    if s.device_index != dev or (stream is not None and torch.cuda.current_device() != dev):
+        raise ValueError(f"the cache is on {cache.k.device}, the stream on cuda:{s.device_index}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+    return s.cuda_stream
 
 
 class KvCache:
@@ -493,8 +516,12 @@ class KvCache:
         _want(table, "table", torch.int32)
         _want(lens, "lens", torch.int32, table.shape[:1])
         self.k, self.v, self.k_scale, self.v_scale, self.table, self.lens = k, v, k_scale, v_scale, table, lens
+        parts = (k, v, k_scale, v_scale, table, lens)
+        if any(t.device != k.device for t in parts):
+            raise ValueError(f"the cache's tensors are on {', '.join(str(t.device) for t in parts)}")
         self.c = CKvCache(lead[0] if len(lead) == 3 else 1, lead[-2], lead[-1], head_dim, 32 * groups, table.shape[1],
-                          table.shape[0], *(t.data_ptr() for t in (k, v, k_scale, v_scale, table, lens)))
+                          table.shape[0], *(t.data_ptr() for t in parts))
+        self.ref, self.device, self.head_dim, self.width = ctypes.byref(self.c), k.get_device(), head_dim, lead[-1] * head_dim
 
     @classmethod
     def empty(cls, n_pages, n_kv_heads, head_dim, page_tokens, table_rows, max_pages, n_blocks=1, device="cuda"):
@@ -515,52 +542,57 @@ def cache_tables(cache: KvCache, lens_before, added, free_pages, runs, counts, n
                  stream=None):
     """lens_before None: every request is new; free_pages None: no page is free."""
     i32 = torch.int32
-    n = _want(added, "added", i32).numel()
-    _want(runs, "runs", i32, (runs.shape[0], 4))
+    n, n_runs = _want(added, "added", i32).numel(), runs.shape[0]
+    _want(runs, "runs", i32, (n_runs, 4))
     _want(counts, "counts", i32, (4,))
     if lens_before is not None:
         _want(lens_before, "lens_before", i32, added.shape)
     n_free = 0 if free_pages is None else _want(free_pages, "free_pages", i32).numel()
-    _check(lib().dit_cache_tables(ctypes.byref(cache.c), n, _ptr(lens_before), _ptr(added), int(rows_per_req), int(n_rows),
-                                  _ptr(free_pages), n_free, _ptr(runs), runs.shape[0], _ptr(counts), _stream(stream)),
-           "dit_cache_tables")
+    s = _cache_stream(cache, stream, lens_before, added, free_pages, runs, counts)
+    _check(lib().dit_cache_tables(cache.ref, n, _at(lens_before), added.data_ptr(), rows_per_req, n_rows, _at(free_pages),
+                                  n_free, runs.data_ptr(), n_runs, counts.data_ptr(), s), "dit_cache_tables")
 
 
 def _rows_of(t, name, width):
-    if t.dim() != 2 or t.stride(1) != 1 or t.shape[1] < width:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}; needed: rows of {width} dense values")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    """The distance between a tensor's rows."""
+    if t.dim() == 2:
+        (rows, cols), (stride, one) = t.shape, t.stride()
+        if one == 1 and cols >= width:
+            return stride if rows > 1 else max(stride, cols)
+    raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}; needed: rows of {width} dense values")
 
 
 def cache_store(cache: KvCache, k, v, runs, block: int = 0, stream=None):
     """k, v: [rows, n_kv_heads * head_dim], of any row stride."""
-    width = cache.c.n_kv_heads * cache.c.head_dim
-    if k.dtype != v.dtype or k.shape[0] != v.shape[0]:
-        raise ValueError(f"k is {k.dtype} with {k.shape[0]} rows, v {v.dtype} with {v.shape[0]}")
-    ks, vs = _rows_of(k, "k", width), _rows_of(v, "v", width)
-    _want(runs, "runs", torch.int32, (runs.shape[0], 4))
-    _check(lib().dit_cache_store(ctypes.byref(cache.c), int(block), _ptr(k), _ptr(v), ks, vs, k.shape[0], _ptr(runs),
-                                 runs.shape[0], dtype_code(k.dtype), _stream(stream)), "dit_cache_store")
+    rows, n_runs = k.shape[0], runs.shape[0]
+    if k.dtype != v.dtype or rows != v.shape[0]:
+        raise ValueError(f"k is {k.dtype} with {rows} rows, v {v.dtype} with {v.shape[0]}")
+    ks, vs = _rows_of(k, "k", cache.width), _rows_of(v, "v", cache.width)
+    _want(runs, "runs", torch.int32, (n_runs, 4))
+    s = _cache_stream(cache, stream, k, v, runs)
+    _check(lib().dit_cache_store(cache.ref, block, k.data_ptr(), v.data_ptr(), ks, vs, rows, runs.data_ptr(), n_runs,
+                                 dtype_code(k.dtype), s), "dit_cache_store")
 
 
 def attention_cached_workspace_size(cache: KvCache, cu_q, n_heads: int, dtype: torch.dtype, max_len: int = 0) -> int:
     cq = _i32(cu_q)
-    return int(lib().dit_attention_cached_workspace_size(ctypes.byref(cache.c), _pi(cq), len(cq) - 1, int(n_heads),
-                                                         int(max_len), dtype_code(dtype)))
+    return int(lib().dit_attention_cached_workspace_size(cache.ref, _pi(cq), len(cq) - 1, int(n_heads), int(max_len),
+                                                         dtype_code(dtype)))
 
 
 def attention_cached(cache: KvCache, q, o, cu_q, n_heads: int, ws=None, block: int = 0, max_len: int = 0,
                      softmax_scale=None, stream=None):
     """softmax_scale None: the library's default, 1/sqrt(head_dim); ws as attention_cached_workspace_size says."""
     cq = _i32(cu_q)
-    width = n_heads * cache.c.head_dim
+    width = n_heads * cache.head_dim
     if q.dtype != o.dtype or min(q.shape[0], o.shape[0]) < cq[-1]:
         raise ValueError(f"q is {q.dtype} with {q.shape[0]} rows, o {o.dtype} with {o.shape[0]}, cu_q ends at {cq[-1]}")
     qs, os_ = _rows_of(q, "q", width), _rows_of(o, "o", width)
-    _check(lib().dit_attention_cached(ctypes.byref(cache.c), int(block), _ptr(q), _ptr(o), qs, os_, _pi(cq), len(cq) - 1,
-                                      int(n_heads), int(max_len), 0.0 if softmax_scale is None else softmax_scale,
-                                      dtype_code(q.dtype), _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0,
-                                      _stream(stream)), "dit_attention_cached")
+    s = _cache_stream(cache, stream, q, o, ws)
+    _check(lib().dit_attention_cached(cache.ref, block, q.data_ptr(), o.data_ptr(), qs, os_,
+                                      cq.__array_interface__["data"][0], len(cq) - 1, n_heads, max_len,
+                                      0.0 if softmax_scale is None else softmax_scale, dtype_code(q.dtype), _at(ws),
+                                      0 if ws is None else ws.numel() * ws.element_size(), s), "dit_attention_cached")
 
 
 def text_kv_cached_workspace_size(cfg: ModelConfig, vl: Varlen) -> int:
@@ -569,20 +601,22 @@ def text_kv_cached_workspace_size(cfg: ModelConfig, vl: Varlen) -> int:
 
 def text_kv_cached(cfg: ModelConfig, w: ModelWeights, vl: Varlen, txt, cache: KvCache, runs, ws, stream=None):
     _want(runs, "runs", torch.int32, (runs.shape[0], 4))
-    _check(lib().dit_text_kv_cached(ctypes.byref(cfg.c), ctypes.byref(w.c), ctypes.byref(vl.c), _ptr(txt),
-                                    ctypes.byref(cache.c), _ptr(runs), runs.shape[0], _ptr(ws),
-                                    ws.numel() * ws.element_size(), _stream(stream)), "dit_text_kv_cached")
+    s = _cache_stream(cache, stream, txt, runs, ws)
+    _check(lib().dit_text_kv_cached(ctypes.byref(cfg.c), ctypes.byref(w.c), ctypes.byref(vl.c), txt.data_ptr(), cache.ref,
+                                    runs.data_ptr(), runs.shape[0], ws.data_ptr(), ws.numel() * ws.element_size(), s),
+           "dit_text_kv_cached")
 
 
 def denoise_cached_workspace_size(cfg: ModelConfig, vl: Varlen, cache: KvCache) -> int:
-    return int(lib().dit_denoise_cached_workspace_size(ctypes.byref(cfg.c), ctypes.byref(vl.c), ctypes.byref(cache.c)))
+    return int(lib().dit_denoise_cached_workspace_size(ctypes.byref(cfg.c), ctypes.byref(vl.c), cache.ref))
 
 
 def denoise_step_cached(cfg: ModelConfig, w: ModelWeights, vl: Varlen, latent, t, dt, cache: KvCache, latent_out, ws,
                         stream=None):
-    _check(lib().dit_denoise_step_cached(ctypes.byref(cfg.c), ctypes.byref(w.c), ctypes.byref(vl.c), _ptr(latent), _ptr(t),
-                                         _ptr(dt), ctypes.byref(cache.c), _ptr(latent_out), _ptr(ws),
-                                         ws.numel() * ws.element_size(), _stream(stream)), "dit_denoise_step_cached")
+    s = _cache_stream(cache, stream, latent, t, dt, latent_out, ws)
+    _check(lib().dit_denoise_step_cached(ctypes.byref(cfg.c), ctypes.byref(w.c), ctypes.byref(vl.c), latent.data_ptr(),
+                                         t.data_ptr(), dt.data_ptr(), cache.ref, latent_out.data_ptr(), ws.data_ptr(),
+                                         ws.numel() * ws.element_size(), s), "dit_denoise_step_cached")
 
 
 # ------------------------------------------------------------ the simulator

@@ -218,3 +218,18 @@ def test_binding_checks_layouts():
         B.attention_cached(c, kv, kv[:5].clone(), [0, 6], 2)
     with pytest.raises(ValueError):
         B.attention_cached(c, kv, kv.bfloat16(), [0, 6], 2)
+
+
+def test_binding_checks_places():
+    """A cache in host memory is made but not used; its tensors lie in one place."""
+    _lib()
+    c = B.KvCache.empty(3, 2, 64, 64, 4, 5, device="cpu")
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    kv = torch.zeros(6, 128)
+    for call in (lambda: B.cache_tables(c, i32(2), i32(2), i32(4), i32(9, 4), i32(4), 10),
+                 lambda: B.cache_store(c, kv, kv, i32(4, 4)),
+                 lambda: B.attention_cached(c, kv, kv.clone(), [0, 6], 2)):
+        with pytest.raises(ValueError, match="not on a GPU"):
+            call()
+    with pytest.raises(ValueError, match="meta"):
+        B.KvCache(c.k, c.v, c.k_scale, c.v_scale, c.table.to("meta"), c.lens)

@@ -503,3 +503,13 @@ def test_attention_repeats(qlens, klens):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(o, first)
+
+
+def test_tensors_elsewhere_are_refused():
+    B, cache, q, cu, H = _case(BF16, 64, 32, 2, 2, [3], [40], seed=3)
+    o = torch.empty_like(q)
+    for bad in (lambda: B.attention_cached(cache, q.cpu(), o, cu, H), lambda: B.attention_cached(cache, q, o.cpu(), cu, H),
+                lambda: B.attention_cached(cache, q, o, cu, H, ws=torch.empty(64, dtype=torch.uint8)),
+                lambda: B.cache_store(cache, q, q, torch.zeros(1, 4, dtype=torch.int32))):
+        with pytest.raises(ValueError, match="a tensor of"):
+            bad()
