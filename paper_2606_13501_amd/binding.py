@@ -487,11 +487,14 @@ def _cache_stream(cache, stream, *tensors):
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"the cache is on {cache.k.device}, a tensor of {t.dtype} {tuple(t.shape)} on {t.device}")
-    s = torch.cuda.current_stream() if stream is None else stream
+    s = torch.accelerator.current_stream() if stream is None else stream
     if s.device_index != dev or (stream is not None and torch.cuda.current_device() != dev):
         raise ValueError(f"the cache is on {cache.k.device}, the stream on cuda:{s.device_index}, the current device is "
                          f"cuda:{torch.cuda.current_device()}")
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    # 0.6 us instead of 2.7 where it is the default stream, whose handle is 0
+    return 0 if s.stream_id == 0 else torch.cuda.current_stream().cuda_stream
 
 
 class KvCache:
