@@ -109,27 +109,46 @@ struct Segment {
 
 // Workgroups are dispatched to the XCDs round-robin.
 //
+// Where a row of the item's request lies: query row / group of its head row % group.
+__device__ __forceinline__ int64_t query_at(const CachedWork& w, const Segment& g, int row, int64_t stride, int hd) {
+  const int token = w.group == 1 ? row : row / w.group;   // (the division by a variable is 25 instructions)
+  return (w.q_start[g.i] + token) * stride + (g.head * w.group + row - token * w.group) * hd;
+}
+
 // shares == 0: each workgroup has one item, and each XCD the same contiguous
 // eighth of every request's items: the row tiles that read the same keys stay
-// on one XCD and share its L2.
+// on one XCD and share its L2.  The requests with the most tokens go first, so
+// that short items fill the last round (only the device knows the lengths): five
+// images on prompts of 18 to 512 tokens, 24 heads, 40.0 -> 38.9 us; where all
+// lengths are equal the wait for them costs, 33.7 -> 34.3 us for four.
 __device__ __forceinline__ bool whole_item(const CachedWork& w, Segment& g) {
-  const int xcd = blockIdx.x % kXcds;
-  int j = blockIdx.x / kXcds;
-  for (int r = 0; r < w.n_req; ++r) {
-    const int n = w.prefix[r + 1] - w.prefix[r];
-    const int lo = (int)((int64_t)xcd * n / kXcds), hi = (int)((int64_t)(xcd + 1) * n / kXcds);
-    if (j < hi - lo) {
-      g.i = r;
-      g.head = (lo + j) / w.tiles[r];
-      g.tile = lo + j - g.head * w.tiles[r];
-      g.u0 = 0;
-      g.u1 = __builtin_amdgcn_readfirstlane(units_of(w, w.req[r]));
-      g.slot = -1;
-      return true;
+  const int xcd = blockIdx.x % kXcds, at = blockIdx.x / kXcds;
+  int item;
+  g.i = 0;
+  if (w.n_req == 1) {   // without waiting for a length
+    const int lo = xcd * w.prefix[1] / kXcds;   // (kMaxItems * 8 fits)
+    item = lo + at;
+    if (item >= (xcd + 1) * w.prefix[1] / kXcds) return false;
+  } else {
+    const int lane = threadIdx.x % kWave, i = min(lane, w.n_req - 1), len = length_of(w, w.req[i]);
+    const int n = w.prefix[i + 1] - w.prefix[i];
+    const int lo = xcd * n / kXcds, mine = (xcd + 1) * n / kXcds - lo;
+    int start = 0;   // items of the requests before this lane's
+    for (int j = 0; j < w.n_req; ++j) {
+      const int lj = __builtin_amdgcn_readlane(len, j), nj = __builtin_amdgcn_readlane(mine, j);
+      start += lj > len || (lj == len && j < i) ? nj : 0;
     }
-    j -= hi - lo;
+    const uint64_t here = __builtin_amdgcn_ballot_w64(lane < w.n_req && at >= start && at < start + mine);
+    if (here == 0) return false;
+    g.i = __builtin_ctzll(here);
+    item = __builtin_amdgcn_readlane(lo + at - start, g.i);
   }
-  return false;
+  g.head = item / w.tiles[g.i];
+  g.tile = item - g.head * w.tiles[g.i];
+  g.u0 = 0;
+  g.u1 = __builtin_amdgcn_readfirstlane(units_of(w, w.req[g.i]));
+  g.slot = -1;
+  return true;
 }
 
 // shares > 0: the units of all items, in order, are dealt evenly to the
@@ -173,17 +192,22 @@ __device__ __forceinline__ bool next_segment(const CachedWork& w, const int64_t*
 }
 
 // Position of a group of 32 tokens in the pool, in groups (its page, head and
-// place in the page), and its two scale bytes; none where the table names no
-// page of the pool.
+// place in the page), and its two scale bytes; none where `is` is false or the
+// table names no page of the pool.  Without branches, and reading the table and
+// the scales in any case (at entries that exist): nothing waits for the length,
+// nor the tokens' loads for the scales.
 constexpr uint32_t kNoGroup = 0xFFFFFFFFu;
-__device__ __forceinline__ uint32_t find_group(const CachedWork& w, int r, int head, int g, uint32_t& scales) {
+struct GroupAt {
+  uint32_t at;
+  uint8_t k_scale, v_scale;
+  __device__ __forceinline__ uint32_t scales() const { return at == kNoGroup ? 0x7F7Fu : k_scale | (uint32_t)v_scale << 8; }
+};
+__device__ __forceinline__ GroupAt find_group(const CachedWork& w, int r, int head, int g, bool is) {
   const int gs = w.page_shift - 5;   // log2 groups per page
-  const int page = w.table[(int64_t)r * w.max_pages + (g >> gs)];
-  scales = 0x7F7Fu;
-  if (page < 0 || page >= w.n_pages) return kNoGroup;
-  const uint32_t slot = (uint32_t)page * w.n_kv_heads + head;
-  scales = w.k_scale[slot] | (uint32_t)w.v_scale[slot] << 8;
-  return (slot << gs) + (g & ((1 << gs) - 1));
+  const int page = w.table[(int64_t)r * w.max_pages + min(g >> gs, w.max_pages - 1)];
+  is &= (uint32_t)page < (uint32_t)w.n_pages;
+  const uint32_t slot = (is ? (uint32_t)page : 0u) * w.n_kv_heads + head;
+  return {is ? (slot << gs) + (g & ((1 << gs) - 1)) : kNoGroup, w.k_scale[slot], w.v_scale[slot]};
 }
 
 // Sum and maximum of a lane's value and that of the lane 32 (or 16) apart.
@@ -385,31 +409,12 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
     const int len = __builtin_amdgcn_readfirstlane(length_of(w, r));
     const int t_begin = it.u0, t_end = it.u1;   // tiles: units of 64 tokens
 
-    // the queries are on their way while the first tiles are looked up
-    bf16x8 raw[HD / 16];
-    {
-      const int row = min(row0 + fr, rows - 1);
-      load_row<HD>(Q + (int64_t)(w.q_start[it.i] + row / w.group) * w.q_stride +
-                       (it.head * w.group + row % w.group) * HD, fh, raw);
-    }
-
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_char*)smem;
     const uint32_t voff = (uint32_t)(wave * 1024 % kGroup + lane * 16);
     // Where the next 64 tiles lie, one per lane: tile chunk0 + i's groups and
     // their scale bytes (keys, values, keys, values).
     int chunk0 = 0;
     uint32_t at0 = kNoGroup, at1 = kNoGroup, scales = 0;
-    auto look_up = [&](int t0, int n) __attribute__((always_inline)) {
-      chunk0 = t0;
-      const int t = t0 + lane;
-      uint32_t s0 = 0x7F7Fu, s1 = 0x7F7Fu;
-      at0 = at1 = kNoGroup;
-      if (lane < n) at0 = find_group(w, r, it.head, 2 * t, s0);
-      if (lane < n && 64 * t + 32 < len) at1 = find_group(w, r, it.head, 2 * t + 1, s1);
-      scales = s0 | s1 << 16;
-      // some group before the request's end is missing
-      return __builtin_amdgcn_ballot_w64(lane < n && (at0 == kNoGroup || (64 * t + 32 < len && at1 == kNoGroup))) != 0;
-    };
     auto issue = [&](int t) __attribute__((always_inline)) {
       const uint32_t lds = lds_base + (uint32_t)((t % kRing) * kSlot + wave * 1024);
 #pragma unroll
@@ -427,16 +432,27 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       }
     };
 
-    // tiles c0 .. c1 - 1 (at most 64) are next: the first ones on their way
-    bool any_bad = false;
-    auto begin_chunk = [&](int c0, int c1) __attribute__((always_inline)) {
-      any_bad = look_up(c0, c1 - c0);
-      __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): only tile loads are counted from here on
-      __syncthreads();                      // the tiles before have been read
+    // tiles c0 .. c1 - 1 (at most 64) are next: the first ones on their way, after
+    // what `before` asks for (behind the lookup, which would wait for it)
+    bool any_bad = false;   // some group before the request's end is missing
+    auto begin_chunk = [&](int c0, int c1, auto before) __attribute__((always_inline)) {
+      chunk0 = c0;
+      const int t = c0 + lane;
+      const bool is0 = t < c1, is1 = is0 && 64 * t + 32 < len;
+      const GroupAt a = find_group(w, r, it.head, 2 * t, is0), b = find_group(w, r, it.head, 2 * t + 1, is1);
+      at0 = a.at;
+      at1 = b.at;
+      any_bad = __builtin_amdgcn_ballot_w64((is0 && at0 == kNoGroup) || (is1 && at1 == kNoGroup)) != 0;
+      __syncthreads();   // the tiles before have been read
+      before();
       const int n = min(4, c1 - c0);
       for (int t = 0; t < n; ++t) issue(c0 + t);
+      scales = a.scales() | b.scales() << 16;
     };
-    begin_chunk(t_begin, min(t_begin + kWave, t_end));
+    bf16x8 raw[HD / 16];
+    begin_chunk(t_begin, min(t_begin + kWave, t_end), [&]() __attribute__((always_inline)) {
+      load_row<HD>(Q + query_at(w, it, min(row0 + fr, rows - 1), w.q_stride, HD), fh, raw);
+    });
     bool begun = true;
     QFrag<HD> q;
     split_row<HD, QNORM>(raw, fh, w, q);
@@ -497,14 +513,9 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       l_run[0] = l_run[1] = 0.f;
       for (int c0 = t_begin; c0 < t_end; c0 += kWave) {
         const int c1 = min(c0 + kWave, t_end);
-        if (!begun) begin_chunk(c0, c1);
+        if (!begun) begin_chunk(c0, c1, [] {});
         begun = false;
-        // tile c0 in LDS
-        const int n_pre = min(4, c1 - c0);
-        if (n_pre == 4) wait_vmcnt<3 * kLoads>();
-        else if (n_pre == 3) wait_vmcnt<2 * kLoads>();
-        else if (n_pre == 2) wait_vmcnt<kLoads>();
-        else wait_vmcnt<0>();
+        wait_vmcnt<0>();   // the first tiles, asked for with the queries and scales; only tile loads are counted from here on
         __syncthreads();
         // tile t is done: tile t + 1 in LDS for every wave; tile t + 4 into the slot of t
         auto advance = [&](int t) __attribute__((always_inline)) {
@@ -633,8 +644,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       const u32x4 x = *reinterpret_cast<const u32x4*>(stage + n * (HD * 2) + ((i ^ (n % kChunks)) * 16));
       const int row = row0 + n;
       if (row < rows)
-        *reinterpret_cast<u32x4*>(O + (int64_t)(w.q_start[it.i] + row / w.group) * w.o_stride +
-                                  (it.head * w.group + row % w.group) * HD + 8 * i) = x;
+        *reinterpret_cast<u32x4*>(O + query_at(w, it, row, w.o_stride, HD) + 8 * i) = x;
     }
     __builtin_amdgcn_wave_barrier();
   } while (SHARES && next_segment(w, ends, share, it));
@@ -652,8 +662,6 @@ __device__ __forceinline__ void join_waves(const float (&o)[WAVES][ROWS][HD + 4]
   for (int e = threadIdx.x; e < min(ROWS, rows - row0) * HD; e += WAVES * kWave) {
     const int i = e / HD, d = e % HD;
     const int row = row0 + i;
-    const int token = w.q_start[it.i] + row / w.group;
-    const int q_head = it.head * w.group + row % w.group;
     float top = -INFINITY;
 #pragma unroll
     for (int v = 0; v < WAVES; ++v)
@@ -671,7 +679,7 @@ __device__ __forceinline__ void join_waves(const float (&o)[WAVES][ROWS][HD + 4]
       w.part[at * HD + d] = acc;
       if (d == 0) *reinterpret_cast<f32x2*>(w.part + (int64_t)2 * w.shares * ROWS * HD + 2 * at) = f32x2{top, sum};
     } else {
-      O[(int64_t)token * w.o_stride + q_head * HD + d] = from_f<T>(sum != 0.f ? acc / sum : 0.f);
+      O[query_at(w, it, row, w.o_stride, HD) + d] = from_f<T>(sum != 0.f ? acc / sum : 0.f);
     }
   }
 }
@@ -707,20 +715,17 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __
     const int r = w.req[it.i];
     const int rows = w.q_len[it.i] * w.group;
     const int row = min(fr, rows - 1);
-    const int token = w.q_start[it.i] + row / w.group;
     const int len = __builtin_amdgcn_readfirstlane(length_of(w, r));
     const int g_begin = 4 * it.u0, g_end = min(4 * it.u1, (len + 31) / 32);   // units of 128 tokens
     const int n_mine = max(0, (g_end - g_begin - wave + WAVES - 1) / WAVES);   // groups g_begin + wave + WAVES i
-
-    bf16x8 raw[HD / 16];
-    load_row<HD>(Q + (int64_t)token * w.q_stride + (it.head * w.group + row % w.group) * HD, fh, raw);
 
     uint32_t at = kNoGroup, scales = 0;   // lane i: this wave's group base + i
     int base = 0;
     auto look_up = [&](int i0) __attribute__((always_inline)) {
       base = i0;
-      at = kNoGroup;
-      if (i0 + lane < n_mine) at = find_group(w, r, it.head, g_begin + wave + WAVES * (i0 + lane), scales);
+      const GroupAt x = find_group(w, r, it.head, g_begin + wave + WAVES * (i0 + lane), i0 + lane < n_mine);
+      at = x.at;
+      scales = x.scales();
     };
     struct Group {
       u32x4 k[2 * NC], v[ND];
@@ -794,12 +799,13 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __
       }
     };
 
-    // the first tokens are on their way before the queries are split
+    // the first tokens are on their way before the queries are split (and looked up
+    // before the queries are asked for: loads come back in their order)
     Group a{};
-    if (n_mine > 0) {
-      look_up(0);
-      fetch(0, a);
-    }
+    bf16x8 raw[HD / 16];
+    look_up(0);
+    load_row<HD>(Q + query_at(w, it, row, w.q_stride, HD), fh, raw);
+    if (n_mine > 0) fetch(0, a);
     split_row<HD, QNORM>(raw, fh, w, q);
     for (int i0 = 0; i0 < n_mine; i0 += kWave) {
       if (i0 > 0) {
@@ -862,14 +868,6 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_f32(const float* _
     const int req = w.req[it.i];
     const int rows = w.q_len[it.i] * w.group;
     const int row = min(it.tile * 16 + r, rows - 1);
-    const float* qp = Q + (int64_t)(w.q_start[it.i] + row / w.group) * w.q_stride +
-                      (it.head * w.group + row % w.group) * HD + 4 * g4;
-    f32x4 q[NB], acc[NB];
-#pragma unroll
-    for (int c = 0; c < NB; ++c) {
-      q[c] = *reinterpret_cast<const f32x4*>(qp + 16 * c);
-      acc[c] = f32x4{};
-    }
     const int len = __builtin_amdgcn_readfirstlane(length_of(w, req));
     const int t_begin = 8 * it.u0, t_end = min(8 * it.u1, (len + 15) / 16);   // units of 128 tokens
     const int n_mine = max(0, (t_end - t_begin - wave + WAVES - 1) / WAVES);   // tiles t_begin + wave + WAVES i
@@ -877,9 +875,18 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_f32(const float* _
     int base = 0;
     auto look_up = [&](int i0) __attribute__((always_inline)) {
       base = i0;
-      at = kNoGroup;
-      if (i0 + lane < n_mine) at = find_group(w, req, it.head, (t_begin + wave + WAVES * (i0 + lane)) / 2, scales);
+      const GroupAt x = find_group(w, req, it.head, (t_begin + wave + WAVES * (i0 + lane)) / 2, i0 + lane < n_mine);
+      at = x.at;
+      scales = x.scales();
     };
+    look_up(0);   // before the queries, for which it would wait
+    const float* qp = Q + query_at(w, it, row, w.q_stride, HD) + 4 * g4;
+    f32x4 q[NB], acc[NB];
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+      q[c] = *reinterpret_cast<const f32x4*>(qp + 16 * c);
+      acc[c] = f32x4{};
+    }
     struct Tile {
       uint32_t k[NB], v[NB];
     };
@@ -940,7 +947,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_f32(const float* _
       m = m_new;
     };
     for (int i0 = 0; i0 < n_mine; i0 += kWave) {
-      look_up(i0);
+      if (i0 > 0) look_up(i0);
       const int n = min(n_mine - i0, kWave);
       Tile a;
       fetch(i0, a);
