@@ -418,7 +418,7 @@ typedef struct {
   int n_blocks, n_pages, n_kv_heads;
   int head_dim;             /* 64 or 128 */
   int page_tokens;          /* 32, 64, 128 or 256 */
-  int max_pages;            /* width of the block table; max_pages * page_tokens < 2^31 */
+  int max_pages;            /* width of the block table; max_pages * page_tokens <= 2^30 */
   int table_rows;           /* requests that the table and lens have room for */
   void *k, *v;              /* device: pools */
   uint8_t *k_scale, *v_scale;

@@ -552,8 +552,8 @@ def cache_tables(cache: KvCache, lens_before, added, free_pages, runs, counts, n
         _want(lens_before, "lens_before", i32, added.shape)
     n_free = 0 if free_pages is None else _want(free_pages, "free_pages", i32).numel()
     s = _cache_stream(cache, stream, lens_before, added, free_pages, runs, counts)
-    _check(lib().dit_cache_tables(cache.ref, n, _at(lens_before), added.data_ptr(), rows_per_req, n_rows, _at(free_pages),
-                                  n_free, runs.data_ptr(), n_runs, counts.data_ptr(), s), "dit_cache_tables")
+    _check(lib().dit_cache_tables(cache.ref, n, _at(lens_before), added.data_ptr(), int(rows_per_req), int(n_rows),
+                                  _at(free_pages), n_free, runs.data_ptr(), n_runs, counts.data_ptr(), s), "dit_cache_tables")
 
 
 def _rows_of(t, name, width):
@@ -573,7 +573,7 @@ def cache_store(cache: KvCache, k, v, runs, block: int = 0, stream=None):
     ks, vs = _rows_of(k, "k", cache.width), _rows_of(v, "v", cache.width)
     _want(runs, "runs", torch.int32, (n_runs, 4))
     s = _cache_stream(cache, stream, k, v, runs)
-    _check(lib().dit_cache_store(cache.ref, block, k.data_ptr(), v.data_ptr(), ks, vs, rows, runs.data_ptr(), n_runs,
+    _check(lib().dit_cache_store(cache.ref, int(block), k.data_ptr(), v.data_ptr(), ks, vs, rows, runs.data_ptr(), n_runs,
                                  dtype_code(k.dtype), s), "dit_cache_store")
 
 
@@ -592,8 +592,8 @@ def attention_cached(cache: KvCache, q, o, cu_q, n_heads: int, ws=None, block: i
         raise ValueError(f"q is {q.dtype} with {q.shape[0]} rows, o {o.dtype} with {o.shape[0]}, cu_q ends at {cq[-1]}")
     qs, os_ = _rows_of(q, "q", width), _rows_of(o, "o", width)
     s = _cache_stream(cache, stream, q, o, ws)
-    _check(lib().dit_attention_cached(cache.ref, block, q.data_ptr(), o.data_ptr(), qs, os_,
-                                      cq.__array_interface__["data"][0], len(cq) - 1, n_heads, max_len,
+    _check(lib().dit_attention_cached(cache.ref, int(block), q.data_ptr(), o.data_ptr(), qs, os_,
+                                      cq.__array_interface__["data"][0], len(cq) - 1, int(n_heads), int(max_len),
                                       0.0 if softmax_scale is None else softmax_scale, dtype_code(q.dtype), _at(ws),
                                       0 if ws is None else ws.numel() * ws.element_size(), s), "dit_attention_cached")
 

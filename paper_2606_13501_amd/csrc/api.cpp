@@ -658,7 +658,7 @@ dit_status check_cache(const dit_kv_cache* c, bool pools, int n_req) {
     if (!c->k_scale || !c->v_scale) return fail(DIT_ERR_INVALID_ARG, "cache k_scale or v_scale is NULL");
   }
   if (n_req > 0) {
-    if (c->max_pages < 1 || (int64_t)c->max_pages * c->page_tokens > 0x7FFFFFFF)
+    if (c->max_pages < 1 || (int64_t)c->max_pages * c->page_tokens > (1 << 30))
       return fail(DIT_ERR_INVALID_ARG, "cache table of %d pages of %d tokens per request", c->max_pages, c->page_tokens);
     if (n_req > c->table_rows) return fail(DIT_ERR_INVALID_ARG, "%d requests, the cache table has %d rows", n_req, c->table_rows);
     DIT_TRY(check_ints(c->table, "cache table")); DIT_TRY(check_ints(c->lens, "cache lens"));

@@ -50,7 +50,7 @@ constexpr int kXcds = 8;
 // numbered with the row tiles of a head side by side.
 struct CachedWork {
   int n_req;
-  int shares;                       // 0: one workgroup per item; else see Segments
+  int shares;                       // 0: one workgroup per item; else see Share
   int unit_shift, min_share;        // log2 tokens of a unit; units
   int tile_rows;
   int n_pages, page_shift, max_pages, max_len;

@@ -46,7 +46,7 @@ BAD_CACHES = [
 BAD_POOLS = [(dict(k=0), BAD, "cache k is NULL"), (dict(v=V + 8), BAD, "cache v is not"), (dict(k_scale=0), BAD, "k_scale"),
              (dict(v_scale=0), BAD, "v_scale")]
 BAD_TABLES = [(dict(table_rows=1), BAD, "table has 1 rows"), (dict(max_pages=0), BAD, "table of 0"),
-              (dict(max_pages=1 << 25), BAD, "cache table of"), (dict(table=0), BAD, "cache table"),
+              (dict(max_pages=1 << 25), BAD, "cache table of"), (dict(max_pages=(1 << 24) + 1), BAD, "cache table of"), (dict(table=0), BAD, "cache table"),
               (dict(lens=0), BAD, "cache lens")]
 
 

@@ -513,3 +513,81 @@ def test_tensors_elsewhere_are_refused():
                 lambda: B.cache_store(cache, q, q, torch.zeros(1, 4, dtype=torch.int32))):
         with pytest.raises(ValueError, match="a tensor of"):
             bad()
+
+
+@pytest.mark.parametrize("dtype,dim", TYPES)
+@pytest.mark.parametrize("most", [1, 40, 150])
+def test_attention_many_requests(dtype, dim, most):
+    """As many requests as a call takes, on equal and different lengths, some
+    without queries, some without tokens."""
+    rng = np.random.default_rng(most)
+    qlens = [int(x) for x in rng.integers(0, most + 1, 64)]
+    klens = [int(x) for x in rng.choice([0, 1, 18, 64, 64, 65, 200, 517], 64)]
+    B, cache, q, cu, H = _case(dtype, dim, 32, 2, 1, qlens, klens, seed=21)
+    _check_attention(cache, q, _attend(B, cache, q, cu, H), cu, H, rows=6)
+
+
+@pytest.mark.parametrize("dtype,dim", TYPES)
+@pytest.mark.parametrize("qlens,klens", [([9], [100]), ([150], [200]), ([9], [3000]), ([200], [3000])])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_attention_bad_query_rows(dtype, dim, qlens, klens, bad):
+    """A query row that is not finite gives a row of NaN, and no other one."""
+    B, cache, q, cu, H = _case(dtype, dim, 64, 2, 1, qlens, klens, seed=22)
+    log(f"  a value of {bad}")
+    q[3, 5] = bad   # of the first head
+    o = _attend(B, cache, q, cu, H)
+    assert o[3, :dim].isnan().all()
+    # the row and head that were spoilt, taken from a call without it
+    q[3, 5] = 0
+    o[3, :dim] = _attend(B, cache, q, cu, H)[3, :dim]
+    _check_attention(cache, q, o, cu, H)
+
+
+def test_two_calls_at_once():
+    """Attention of two batches on two streams, each with its own workspace,
+    while a third stream writes another request's pages."""
+    B, cache, q, cu, H = _case(BF16, 128, 64, 4, 1, [300, 40], [4000, 700], seed=23)
+    spare = int(np.setdiff1d(np.arange(cache.c.n_pages), cache.table.cpu().numpy())[0])   # of neither
+    x, _ = _bits(np.random.default_rng(24).standard_normal((64, 4 * 128)), BF16)
+    runs = _i32([(spare, 0, 0, 64)])
+    few, cu_few = q[:2].contiguous(), [0, 1, 2]
+    want = _attend(B, cache, q, cu, H), _attend(B, cache, few, cu_few, H)
+    outs = [torch.empty_like(want[0]), torch.empty_like(want[1])]
+    ws = [torch.empty(max(B.attention_cached_workspace_size(cache, c, H, BF16), 256), dtype=torch.uint8, device="cuda")
+          for c in (cu, cu_few)]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for rep in range(20):
+        B.attention_cached(cache, q, outs[0], cu, H, ws[0], stream=streams[0])
+        B.attention_cached(cache, few, outs[1], cu_few, H, ws[1], stream=streams[1])
+        B.cache_store(cache, x, x, runs, stream=streams[2])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_padded_batch_into_the_cache(dtype):
+    """Requests' rows at equal distances, the rows behind each one's tokens NaN:
+    the same pages as from packed rows."""
+    B = require_gpu()
+    log(f"case padded batch {dtype}")
+    rng = np.random.default_rng(25)
+    P, H, d, per, added = 32, 3, 64, 50, [50, 0, 33, 7]
+    n = len(added)
+    packed, _ = _bits(rng.standard_normal((sum(added), H * d)), dtype)
+    padded = torch.full((n * per, H * d), float("nan"), dtype=dtype, device="cuda")
+    at = 0
+    for r, a in enumerate(added):
+        padded[r * per:r * per + a] = packed[at:at + a]
+        at += a
+    caches = []
+    for x, rows_per in ((packed, 0), (padded, per)):
+        cache = B.KvCache.empty(8, H, d, P, n, 2)
+        runs = torch.empty((B.cache_run_bound(P, n, x.shape[0]), 4), dtype=torch.int32, device="cuda")
+        counts = _i32([0] * 4)
+        B.cache_tables(cache, None, _i32(added), _i32([7, 1, 4, 2, 0, 3]), runs, counts, x.shape[0], rows_per)
+        assert counts.tolist() == [5, 5, 0, sum(added)]
+        B.cache_store(cache, x, x, runs)
+        caches.append(cache)
+    for a, b in zip(*((c.k, c.v, c.k_scale, c.v_scale, c.table, c.lens) for c in caches)):
+        assert torch.equal(a, b)
