@@ -537,9 +537,11 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
                 if ((t ^ (blockIdx.x >> 8)) & 1) __builtin_amdgcn_s_setprio(1);
                 else __builtin_amdgcn_s_setprio(0);
               }
-              f32x16 s[2];
-              scores(t, s);
-              output(t, s);
+              if (row0 < rows) {
+                f32x16 s[2];
+                scores(t, s);
+                output(t, s);
+              }
               advance(t);
             }
             if (t >= c1) break;
