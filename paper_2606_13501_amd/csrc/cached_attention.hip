@@ -52,7 +52,8 @@ struct CachedWork {
   int n_req;
   int shares;                       // 0: one workgroup per item; else see Share
   int unit_shift, min_share;        // log2 tokens of a unit; units
-  int tile_rows;
+  int extra;                        // what an item costs beside its tokens, in units
+  int tile_rows, merge_rows;
   int n_pages, page_shift, max_pages, max_len;
   int n_heads, n_kv_heads, group;   // group: query heads of a key/value head
   int64_t q_stride, o_stride;
@@ -75,12 +76,15 @@ __device__ __forceinline__ int units_of(const CachedWork& w, int r) {
   return (length_of(w, r) + (1 << w.unit_shift) - 1) >> w.unit_shift;
 }
 
-// ends[i] = units (of tokens, over all items) of requests 0 .. i; by the first
-// wave, for the workgroup.
+// What an item of the request costs, in units; one without tokens is left to
+// cached_attn_merge.
+__device__ __forceinline__ int cost_of(const CachedWork& w, int units) { return units > 0 ? units + w.extra : 0; }
+
+// ends[i] = cost of requests 0 .. i; by the first wave, for the workgroup.
 __device__ __forceinline__ void count_units(const CachedWork& w, int64_t* ends) {
   if (threadIdx.x < kWave) {
     const int i = threadIdx.x;
-    int64_t v = i < w.n_req ? (int64_t)w.tiles[i] * w.n_kv_heads * units_of(w, w.req[i]) : 0;
+    int64_t v = i < w.n_req ? (int64_t)w.tiles[i] * w.n_kv_heads * cost_of(w, units_of(w, w.req[i])) : 0;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
       const int64_t below = __shfl_up(v, o, kWave);
@@ -151,12 +155,13 @@ __device__ __forceinline__ bool whole_item(const CachedWork& w, Segment& g) {
   return true;
 }
 
-// shares > 0: the units of all items, in order, are dealt evenly to the
-// workgroups, as many as run at once: workgroup s has units s * share ..
-// (s + 1) * share, so all end together whatever the requests' lengths, which
-// only the device knows.  An item that lies in several shares is joined by
-// cached_attn_merge; a share has at most one item that began before it (slot
-// 2 s) and one that ends after it (slot 2 s + 1).
+// shares > 0: the costs of all items, in order, are dealt evenly to the
+// workgroups, as many as run at once, so that all end together whatever the
+// requests' lengths, which only the device knows.  An item's cost is its units
+// and, before them, `extra` units for what every piece of work takes besides: a
+// share of one long item is not behind one of many short ones.  An item that
+// lies in several shares is joined by cached_attn_merge; a share has at most one
+// item that began before it (slot 2 s) and one that ends after it (slot 2 s + 1).
 struct Share {
   int s;
   int64_t pos, end;
@@ -171,24 +176,28 @@ __device__ __forceinline__ Share my_share(const CachedWork& w, int64_t* ends) {
   return x;
 }
 __device__ __forceinline__ bool next_segment(const CachedWork& w, const int64_t* ends, Share& x, Segment& g) {
-  if (x.pos >= x.end) return false;
-  int64_t start = 0, upto = uniform(ends[0]);
-  int r = 0;
-  while (upto <= x.pos) {
-    start = upto;
-    upto = uniform(ends[++r]);
+  while (x.pos < x.end) {
+    int64_t start = 0, upto = uniform(ends[0]);
+    int r = 0;
+    while (upto <= x.pos) {
+      start = upto;
+      upto = uniform(ends[++r]);
+    }
+    const int units = __builtin_amdgcn_readfirstlane(units_of(w, w.req[r]));
+    const int cost = cost_of(w, units);
+    const int64_t item = uniform((x.pos - start) / cost);
+    const int from = (int)(x.pos - start - item * cost), to = (int)min((int64_t)cost, from + x.end - x.pos);
+    x.pos += to - from;
+    g.u0 = max(from - w.extra, 0);
+    g.u1 = max(to - w.extra, 0);
+    if (g.u1 == g.u0) continue;
+    g.i = r;
+    g.head = __builtin_amdgcn_readfirstlane((int)(item / w.tiles[r]));
+    g.tile = (int)(item - (int64_t)g.head * w.tiles[r]);
+    g.slot = g.u1 - g.u0 == units ? -1 : 2 * x.s + (g.u0 == 0);
+    return true;
   }
-  const int units = __builtin_amdgcn_readfirstlane(units_of(w, w.req[r]));
-  const int64_t item = uniform((x.pos - start) / units);
-  g.i = r;
-  g.u0 = (int)(x.pos - start - item * units);
-  const int n = (int)min((int64_t)(units - g.u0), x.end - x.pos);
-  g.u1 = g.u0 + n;
-  g.head = __builtin_amdgcn_readfirstlane((int)(item / w.tiles[r]));
-  g.tile = (int)(item - (int64_t)g.head * w.tiles[r]);
-  g.slot = n == units ? -1 : 2 * x.s + (g.u0 == 0);
-  x.pos += n;
-  return true;
+  return false;
 }
 
 // Position of a group of 32 tokens in the pool, in groups (its page, head and
@@ -980,16 +989,30 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_f32(const float* _
 // here.  A workgroup has up to 16 rows of one item, so that the search for its
 // parts, with its divisions, is done once; four channels per thread and row.
 // (With each thread searching for its row: 28 us for 62,400 rows of 2 parts, now
-// 21; 8 rows per workgroup cost 2 us more there, 32 rows 2.5 us more where 10,240
-// rows have 6 parts.)
-constexpr int kMergeRows = 16;
+// 21.)  Where a row has many parts the thread groups of a workgroup share them
+// (105 rows x 25,649 tokens x 6 heads, 50 parts: 57 -> 34 us with it and the
+// even costs).
+struct Joined {
+  float top, l;
+  f32x4 o;
+};
+__device__ __forceinline__ void join(Joined& x, float top, float l, f32x4 o) {
+  if (l == 0.f) return;   // no keys there
+  const float m = fmaxf(x.top, top);
+  const float a = exp2f(x.top - m), b = exp2f(top - m);   // (the first: 2^-inf = 0)
+  x.l = fmaf(b, l, x.l * a);
+  x.o = x.o * a + o * b;
+  x.top = m;
+}
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void cached_attn_merge(T* __restrict__ O, CachedWork w) {
+  constexpr int LANES = HD / 4, GROUPS = 256 / LANES;   // lanes of a row, rows at a time
   __shared__ int64_t ends[kWave];
+  __shared__ Joined halves[GROUPS][LANES];
   count_units(w, ends);
-  const int per_item = (w.tile_rows + kMergeRows - 1) / kMergeRows;
-  const int item = blockIdx.x / per_item, at0 = blockIdx.x % per_item * kMergeRows;
-  const int lane = threadIdx.x % kWave;
+  const int per_item = w.tile_rows / w.merge_rows;
+  const int item = blockIdx.x / per_item, at0 = blockIdx.x % per_item * w.merge_rows;
+  const int lane = threadIdx.x % kWave, group = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
   Segment it;
   it.i = (int)__popcll(__builtin_amdgcn_ballot_w64(lane < w.n_req && w.prefix[min(lane, w.n_req - 1) + 1] <= item));
   const int nth = item - w.prefix[it.i];
@@ -998,44 +1021,52 @@ __global__ __launch_bounds__(256) void cached_attn_merge(T* __restrict__ O, Cach
   const int units = __builtin_amdgcn_readfirstlane(units_of(w, w.req[it.i]));
   int s0 = 0, s1 = -1;
   if (units > 0) {
-    const int64_t first = uniform((it.i > 0 ? ends[it.i - 1] : 0) + (int64_t)nth * units);
+    const int64_t first = uniform((it.i > 0 ? ends[it.i - 1] : 0) + (int64_t)nth * cost_of(w, units) + w.extra);
     const int64_t share = uniform(share_of(w, ends[kWave - 1]));
     s0 = (int)(first / share);
     s1 = (int)((first + units - 1) / share);
     if (s0 == s1) return;   // written by its workgroup
   }
   const f32x2* ml = reinterpret_cast<const f32x2*>(w.part + (int64_t)2 * w.shares * w.tile_rows * HD);
-  const int row0 = it.tile * w.tile_rows;
-  const int n = min(min(w.tile_rows, at0 + kMergeRows), w.q_len[it.i] * w.group - row0);   // rows at0 .. n - 1 of the tile
-  for (int e = threadIdx.x; e < (n - at0) * (HD / 4); e += 256) {
-    const int at = at0 + e / (HD / 4), d = e % (HD / 4) * 4;
-    f32x4 o{};
-    // four parts' loads at a time, joined in order
-    float top = -INFINITY, l = 0.f;
-    for (int s = s0; s <= s1; s += 4) {
+  // parts a .. b of row `at` of the tile, four parts' loads at a time, joined in order
+  auto parts = [&](int at, int a, int b) __attribute__((always_inline)) {
+    Joined y = {-INFINITY, 0.f, f32x4{}};
+    for (int s = a; s <= b; s += 4) {
       f32x2 x[4];
       f32x4 v[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int at_s = min(s + k, s1);
+        const int at_s = min(s + k, b);
         const int64_t slot_row = (int64_t)(2 * at_s + (at_s == s0)) * w.tile_rows + at;
         x[k] = ml[slot_row];
         v[k] = *reinterpret_cast<const f32x4*>(w.part + slot_row * HD + d);
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (s + k > s1 || x[k][1] == 0.f) continue;   // no such part, or one without keys
-        const float m = fmaxf(top, x[k][0]);
-        const float a = exp2f(top - m), b = exp2f(x[k][0] - m);   // (the first: 2^-inf = 0)
-        l = fmaf(b, x[k][1], l * a);
-        o = o * a + v[k] * b;
-        top = m;
-      }
+      for (int k = 0; k < 4; ++k)
+        if (s + k <= b) join(y, x[k][0], x[k][1], v[k]);
     }
-    o *= l != 0.f ? 1.0f / l : 0.f;
-    T* op = O + query_at(w, it, row0 + at, w.o_stride, HD) + d;
+    return y;
+  };
+  auto write = [&](int row, const Joined& y) __attribute__((always_inline)) {
+    const f32x4 o = y.o * (y.l != 0.f ? 1.0f / y.l : 0.f);
+    T* op = O + query_at(w, it, row, w.o_stride, HD) + d;
 #pragma unroll
     for (int j = 0; j < 4; ++j) op[j] = from_f<T>(o[j]);
+  };
+  const int row0 = it.tile * w.tile_rows;
+  const int n = min(at0 + w.merge_rows, w.q_len[it.i] * w.group - row0);   // rows at0 .. n - 1 of the tile
+  if (w.merge_rows >= GROUPS) {
+    for (int at = at0 + group; at < n; at += GROUPS) write(row0 + at, parts(at, s0, s1));
+  } else {
+    const int per_row = GROUPS / w.merge_rows, at = at0 + group / per_row, g0 = group % per_row;
+    const int each = (s1 - s0 + per_row) / per_row, a = s0 + g0 * each;
+    if (at < n) halves[group][d / 4] = parts(at, a, min(a + each - 1, s1));
+    __syncthreads();
+    if (at < n && g0 == 0) {
+      Joined y = halves[group][d / 4];
+      for (int g = 1; g < per_row; ++g) join(y, halves[group + g][d / 4].top, halves[group + g][d / 4].l, halves[group + g][d / 4].o);
+      write(row0 + at, y);
+    }
   }
 }
 
@@ -1045,9 +1076,10 @@ constexpr int64_t kMaxItems = (1 << 22);   // 512 threads each: a launch of fewe
 
 enum Shape { kMany, kFew, kF32 };
 
+
 struct CachedPlan {
   Shape shape;
-  int tile_rows, unit_shift, min_share, shares;
+  int tile_rows, unit_shift, min_share, extra, shares, merge_rows;
 };
 
 // The kernel, and whether its workgroups take whole items or even shares of all
@@ -1055,6 +1087,13 @@ struct CachedPlan {
 // items than four rounds of workgroups, and lengths that may pass 1,024 tokens
 // (below, the joining kernel costs more than the last round).  The bound of the
 // lengths stands for the lengths, which are device memory.
+//
+// A share has at least 256 tokens (with 512, 42 rows x 3,628 tokens x 6 heads
+// took 20 us, now 16).  An item's cost beside its tokens, the latencies of
+// finding and loading its first ones and of writing its part (9 us where a tile
+// of 64 takes 1), is counted as 512 tokens, 1,536 where the waves share the
+// tokens: 13 requests of 3 to 31,478 tokens, 1 to 6 queries of 30 / 6 heads,
+// take 44 us, without it 115.
 CachedPlan plan(const CachedAttnArgs& p, int cus) {
   CachedPlan pl;
   const int group = p.n_heads / p.n_kv_heads;
@@ -1069,15 +1108,20 @@ CachedPlan plan(const CachedAttnArgs& p, int cus) {
   pl.shape = p.dtype == DIT_F32 ? kF32 : most <= 32 ? kFew : kMany;
   pl.tile_rows = pl.shape == kF32 ? 16 : pl.shape == kFew ? 32 : 128;
   pl.unit_shift = pl.shape == kMany ? 6 : 7;
-  pl.min_share = 512 >> pl.unit_shift;
+  pl.min_share = 256 >> pl.unit_shift;
+  pl.extra = pl.shape == kMany ? 8 : 12;
   pl.shares = 0;
   const int64_t items = tiles(pl.tile_rows) * p.n_kv_heads;
   // workgroups that run at once, a multiple of the XCDs
   const int64_t slots = (pl.shape == kMany ? 2 : 1) * (int64_t)std::max(cus / kXcds * kXcds, kXcds);
   if (p.max_len > 1024 && items > 0 && items < 4 * slots) {
-    const int64_t units = items * ((p.max_len + (1 << pl.unit_shift) - 1) >> pl.unit_shift);
+    const int64_t units = items * (((p.max_len + (1 << pl.unit_shift) - 1) >> pl.unit_shift) + pl.extra);
     pl.shares = (int)std::min(slots, ((units + pl.min_share - 1) / pl.min_share + kXcds - 1) / kXcds * kXcds);
   }
+  // joining: up to 8 parts a row by one thread group, more by 2, 4 or 8 of the
+  // workgroup's (1024 / head_dim) groups
+  pl.merge_rows = 16;
+  for (int g = 2; 4 * g * items <= pl.shares && pl.merge_rows > 1; g *= 2) pl.merge_rows = 1024 / p.head_dim / g;
   return pl;
 }
 
@@ -1091,7 +1135,8 @@ size_t cached_attention_ws(const CachedAttnArgs& p) {
 hipError_t launch_cached_attention(const CachedAttnArgs& p, void* ws, hipStream_t s) {
   const CachedPlan pl = plan(p, cu_count());
   CachedWork w{};
-  w.shares = pl.shares; w.unit_shift = pl.unit_shift; w.min_share = pl.min_share; w.tile_rows = pl.tile_rows;
+  w.shares = pl.shares; w.unit_shift = pl.unit_shift; w.min_share = pl.min_share; w.extra = pl.extra;
+  w.tile_rows = pl.tile_rows; w.merge_rows = pl.merge_rows;
   w.n_pages = p.n_pages; w.page_shift = p.page_shift; w.max_pages = p.max_pages; w.max_len = p.max_len;
   w.n_heads = p.n_heads; w.n_kv_heads = p.n_kv_heads; w.group = p.n_heads / p.n_kv_heads;
   w.q_stride = p.q_stride; w.o_stride = p.o_stride;
@@ -1137,7 +1182,7 @@ hipError_t launch_cached_attention(const CachedAttnArgs& p, void* ws, hipStream_
     else if (p.q_gain) cached_attn_many<HD, true, SHARES><<<grid, 256, 0, s>>>(q, o, w);
     else cached_attn_many<HD, false, SHARES><<<grid, 256, 0, s>>>(q, o, w);
     if constexpr (SHARES) {
-      const unsigned blocks = (unsigned)items * ((pl.tile_rows + kMergeRows - 1) / kMergeRows);
+      const unsigned blocks = (unsigned)items * (pl.tile_rows / pl.merge_rows);
       if (pl.shape == kF32) cached_attn_merge<HD, float><<<blocks, 256, 0, s>>>((float*)p.o, w);
       else cached_attn_merge<HD, bf16><<<blocks, 256, 0, s>>>(o, w);
     }
