@@ -856,9 +856,13 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __
 // S^T = K Q^T on 16 keys leaves a lane four keys of one query, which feed O^T =
 // V^T P^T from its registers.  A lane's four codes of an operand are one dword
 // of the page, converted exactly.  Latency-bound at the small configuration's
-// sizes: the next tile is asked for before the last is computed.
+// sizes (64 queries x 77 tokens x 6 heads of 64: 7.5 us): the next tile is asked
+// for before the last is computed.  With many items the fp32 matrix rate is what
+// is left (400 x 512 tokens x 40 heads of 128: 66 us, 30 us of it in matrix
+// instructions); two workgroups per compute unit, at the price of two spilled
+// registers, took it there from 87.
 template <int HD, bool SHARES>
-__global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_f32(const float* __restrict__ Q, float* __restrict__ O,
+__global__ __launch_bounds__(64 * kKeyWaves, SHARES ? 2 : 4) void cached_attn_f32(const float* __restrict__ Q, float* __restrict__ O,
                                                                   CachedWork w) {
   constexpr int NB = HD / 16, kGroup = 32 * HD, WAVES = kKeyWaves;
   __shared__ __attribute__((aligned(16))) float part_o[WAVES][16][HD + 4];
