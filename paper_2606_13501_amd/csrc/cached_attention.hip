@@ -162,6 +162,12 @@ __device__ __forceinline__ bool whole_item(const CachedWork& w, Segment& g) {
 // share of one long item is not behind one of many short ones.  An item that
 // lies in several shares is joined by cached_attn_merge; a share has at most one
 // item that began before it (slot 2 s) and one that ends after it (slot 2 s + 1).
+// A share is worked off from its end: it begins with the item that ends after it,
+// at that item's first token, so the workgroups that read one head's tokens,
+// their shares about an item long, are at the same tokens at the same time, and
+// one XCD's L2 serves them (from its beginning, each a little further on than
+// the last, 1,560 x 31,200 tokens x 40 heads read 3.6 GB past the L2 and took
+// 912 us; now 0.39 GB and 856 us).
 struct Share {
   int s;
   int64_t pos, end;
@@ -179,15 +185,16 @@ __device__ __forceinline__ bool next_segment(const CachedWork& w, const int64_t*
   while (x.pos < x.end) {
     int64_t start = 0, upto = uniform(ends[0]);
     int r = 0;
-    while (upto <= x.pos) {
+    while (upto < x.end) {
       start = upto;
       upto = uniform(ends[++r]);
     }
     const int units = __builtin_amdgcn_readfirstlane(units_of(w, w.req[r]));
     const int cost = cost_of(w, units);
-    const int64_t item = uniform((x.pos - start) / cost);
-    const int from = (int)(x.pos - start - item * cost), to = (int)min((int64_t)cost, from + x.end - x.pos);
-    x.pos += to - from;
+    const int64_t item = uniform((x.end - 1 - start) / cost);
+    const int64_t begin = start + item * cost;
+    const int from = (int)max(x.pos - begin, (int64_t)0), to = (int)(x.end - begin);
+    x.end = begin + from;
     g.u0 = max(from - w.extra, 0);
     g.u1 = max(to - w.extra, 0);
     if (g.u1 == g.u0) continue;
