@@ -390,8 +390,9 @@ constexpr float kHeadroom = 18446744073709551616.0f;   // 2^64, bound of a row s
 // again, so the result is the softmax in any case.
 //
 // Bound by the matrix instructions at the clock that the power limit leaves:
-// at 2,048 queries x 31,200 tokens x 32 heads of 128 the matrix cores are busy
-// for 68% of the cycles at 1.80 GHz.  Other orders of the same instructions
+// 2,048 queries x 31,200 tokens x 32 heads of 128 take 832 us, 1.26 PFLOP/s.
+// (Before a head's workgroups read the same tokens together, 907 us, the matrix
+// cores were busy for 68% of the cycles at 1.80 GHz.)  Other orders of the same instructions
 // reach 74% at 1.74 GHz (the next tile's score products dealt among this one's
 // softmax) or 50% at 2.0 GHz (64 rows per wave, one workgroup per compute unit)
 // and take as long or longer.
@@ -547,8 +548,8 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
             const int t_full = min(c1, len / 64);   // whole tiles
             for (; t < t_full; ++t) {
               // The older of two waves goes first wherever both could; with turns at a higher
-              // priority the compute unit's two workgroups end more nearly together (1,063 ->
-              // 1,035 us at the size above; with whole items it made no difference)
+              // priority the compute unit's two workgroups end more nearly together (849 ->
+              // 833 us at the size above; with whole items it made no difference)
               if constexpr (SHARES) {
                 if ((t ^ (blockIdx.x >> 8)) & 1) __builtin_amdgcn_s_setprio(1);
                 else __builtin_amdgcn_s_setprio(0);
