@@ -1099,10 +1099,14 @@ struct CachedPlan {
 };
 
 // The kernel, and whether its workgroups take whole items or even shares of all
-// tokens.  Shares pay where whole items would leave compute units idle: fewer
-// items than four rounds of workgroups, and lengths that may pass 1,024 tokens
-// (below, the joining kernel costs more than the last round).  The bound of the
-// lengths stands for the lengths, which are device memory.
+// tokens: whichever an estimate from measured times finds shorter.  Shares cost
+// a write, a read and a kernel of joining; whole items leave compute units idle
+// in the last round.  Measured, shares / whole: 1,560 rows x 31,200 tokens x 40
+// heads 846 / 1,153 us, 256 x 8,192 x 40 61 / 128, 3,000 x 1,500 x 40 117 / 96,
+// 700 x 1,500 x 24 40 / 31, single queries on 4,000 tokens x 40 18.6 / 23.8, on
+// 1,200 14.2 / 12.4.  (Within 5% of each other the estimate may miss: 6,000 x
+// 6,000 x 40 654 / 634.)  The bound of the lengths stands for the lengths, which
+// are device memory.
 //
 // A share has at least 256 tokens (with 512, 42 rows x 3,628 tokens x 6 heads
 // took 20 us, now 16).  An item's cost beside its tokens, the latencies of
@@ -1129,10 +1133,20 @@ CachedPlan plan(const CachedAttnArgs& p, int cus) {
   pl.shares = 0;
   const int64_t items = tiles(pl.tile_rows) * p.n_kv_heads;
   // workgroups that run at once, a multiple of the XCDs
-  const int64_t slots = (pl.shape == kMany ? 2 : 1) * (int64_t)std::max(cus / kXcds * kXcds, kXcds);
-  if (p.max_len > 1024 && items > 0 && items < 4 * slots) {
-    const int64_t units = items * (((p.max_len + (1 << pl.unit_shift) - 1) >> pl.unit_shift) + pl.extra);
-    pl.shares = (int)std::min(slots, ((units + pl.min_share - 1) / pl.min_share + kXcds - 1) / kXcds * kXcds);
+  const int64_t cu = std::max(cus / kXcds * kXcds, kXcds), slots = (pl.shape == kMany ? 2 : 1) * cu;
+  const int64_t n = ((int64_t)p.max_len + (1 << pl.unit_shift) - 1) >> pl.unit_shift;
+  if (items > 0 && items <= kMaxItems) {
+    const int64_t units = items * (n + pl.extra);
+    const int64_t shares = std::min(slots, ((units + pl.min_share - 1) / pl.min_share + kXcds - 1) / kXcds * kXcds);
+    // us: of a workgroup beside its units; of a unit, with one workgroup per compute unit and with all; of joining
+    const bool many = pl.shape == kMany;
+    const double fixed = 9, alone = many ? 1.05 : pl.shape == kFew ? 0.5 : 1, full = many ? 1.75 : 1;
+    const double joining = many ? 6 + 14.0 * shares / slots : 5;
+    const int64_t rest = items % slots;
+    const double whole = (items / slots) * (fixed + n * full) + (rest > 0 ? fixed + n * (rest > cu ? full : alone) : 0);
+    const double share = std::max((double)units / shares, (double)pl.min_share);
+    const double even = fixed + share * (shares > cu ? full : alone) + joining;
+    if (even < whole) pl.shares = (int)shares;
   }
   // joining: up to 8 parts a row by one thread group, more by 2, 4 or 8 of the
   // workgroup's (1024 / head_dim) groups
