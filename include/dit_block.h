@@ -473,8 +473,9 @@ dit_status dit_cache_store(const dit_kv_cache *cache, int block, const void *k, 
  * dtypes) and n_kv_heads, a divisor of n_heads, are the cache's.  A request
  * without tokens gets rows of zeros; table rows from n_req on are not read.
  * max_len bounds the lengths (0: the table's width): longer requests are cut
- * there, and the work is divided by it.  Few queries over many tokens divide
- * the tokens among workgroups and join them in the workspace: ws holds
+ * there, and the work is divided by it.  Where whole row tiles would leave
+ * compute units idle, the tokens are divided among the workgroups and what
+ * they find is joined in the workspace: ws holds
  * dit_attention_cached_workspace_size bytes, 256-byte aligned (0 bytes: NULL
  * will do), its contents are scratch, and calls that may overlap in time, or
  * captured graphs that may, each need their own. */

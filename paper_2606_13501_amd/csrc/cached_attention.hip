@@ -111,14 +111,14 @@ struct Segment {
   int slot;            // where its unfinished rows go (-1: it has all of the item's tokens)
 };
 
-// Workgroups are dispatched to the XCDs round-robin.
-//
 // Where a row of the item's request lies: query row / group of its head row % group.
 __device__ __forceinline__ int64_t query_at(const CachedWork& w, const Segment& g, int row, int64_t stride, int hd) {
   const int token = w.group == 1 ? row : row / w.group;   // (the division by a variable is 25 instructions)
   return (w.q_start[g.i] + token) * stride + (g.head * w.group + row - token * w.group) * hd;
 }
 
+// Workgroups are dispatched to the XCDs round-robin.
+//
 // shares == 0: each workgroup has one item, and each XCD the same contiguous
 // eighth of every request's items: the row tiles that read the same keys stay
 // on one XCD and share its L2.  The requests with the most tokens go first, so
@@ -392,10 +392,12 @@ constexpr float kHeadroom = 18446744073709551616.0f;   // 2^64, bound of a row s
 // Bound by the matrix instructions at the clock that the power limit leaves:
 // 2,048 queries x 31,200 tokens x 32 heads of 128 take 832 us, 1.26 PFLOP/s.
 // (Before a head's workgroups read the same tokens together, 907 us, the matrix
-// cores were busy for 68% of the cycles at 1.80 GHz.)  Other orders of the same instructions
-// reach 74% at 1.74 GHz (the next tile's score products dealt among this one's
-// softmax) or 50% at 2.0 GHz (64 rows per wave, one workgroup per compute unit)
-// and take as long or longer.
+// cores were busy for 68% of the cycles at 1.80 GHz.  Other orders of the same
+// instructions reached 74% at 1.74 GHz, the next tile's score products dealt
+// among this one's softmax, or 50% at 2.0 GHz, 64 rows per wave and one
+// workgroup per compute unit, and took as long or longer.)  Short prompts: the
+// first tokens and rows are waited for most of half the time; 32,760 queries x
+// 512 tokens x 40 heads of 128 take 388 us, 0.89 PFLOP/s and 1.7 TB/s.
 template <int HD, bool QNORM, bool SHARES>
 __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restrict__ Q, bf16* __restrict__ O,
                                                            CachedWork w) {
@@ -716,6 +718,10 @@ constexpr int kKeyWaves = 8;   // waves of a workgroup whose waves share the tok
 // tokens of its segment, straight from global memory into registers in the
 // operands' order (whole KiB per load), two groups ahead, with an exact online
 // softmax; the waves meet in LDS, the shares in cached_attn_merge.
+//
+// HBM-bound on long histories: 16 single queries x 2,767 .. 32,760 tokens, 40
+// heads on 8, take 121 us, 5.2 TB/s.  Latency-bound on one prompt: 1 query x 512
+// tokens x 40 heads 9.0 us (the kernel above: 12.4; at 32 rows 11.6 and 13.1).
 template <int HD, bool QNORM, bool SHARES>
 __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __restrict__ Q, bf16* __restrict__ O,
                                                                   CachedWork w) {
@@ -870,7 +876,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __
 // of the page, converted exactly.  Latency-bound at the small configuration's
 // sizes (64 queries x 77 tokens x 6 heads of 64: 7.5 us): the next tile is asked
 // for before the last is computed.  With many items the fp32 matrix rate is what
-// is left (400 x 512 tokens x 40 heads of 128: 66 us, 30 us of it in matrix
+// is left (400 x 512 tokens x 40 heads of 128: 59 us, 30 us of it in matrix
 // instructions); two workgroups per compute unit, at the price of two spilled
 // registers, took it there from 87.
 template <int HD, bool SHARES>
@@ -1135,7 +1141,7 @@ CachedPlan plan(const CachedAttnArgs& p, int cus) {
   // workgroups that run at once, a multiple of the XCDs
   const int64_t cu = std::max(cus / kXcds * kXcds, kXcds), slots = (pl.shape == kMany ? 2 : 1) * cu;
   const int64_t n = ((int64_t)p.max_len + (1 << pl.unit_shift) - 1) >> pl.unit_shift;
-  if (items > 0 && items <= kMaxItems) {
+  if (items > 0 && items < 8 * slots) {   // (of more, the last round is little)
     const int64_t units = items * (n + pl.extra);
     const int64_t shares = std::min(slots, ((units + pl.min_share - 1) / pl.min_share + kXcds - 1) / kXcds * kXcds);
     // us: of a workgroup beside its units; of a unit, with one workgroup per compute unit and with all; of joining
