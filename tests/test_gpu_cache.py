@@ -591,3 +591,15 @@ def test_padded_batch_into_the_cache(dtype):
         caches.append(cache)
     for a, b in zip(*((c.k, c.v, c.k_scale, c.v_scale, c.table, c.lens) for c in caches)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,dim", TYPES)
+@pytest.mark.parametrize("qlens,klens", [([1] * 12, [9000, 3, 3, 0, 1, 159, 136, 4000, 32, 58, 2, 17]),
+                                         ([2, 1, 1, 3], [1, 1, 1, 7000]), ([40, 33, 1, 50], [6000, 3, 0, 900]),
+                                         ([129, 1], [64, 8000]), ([1], [20000])])
+def test_attention_short_beside_long(dtype, dim, qlens, klens):
+    """Shares that hold many short requests, parts of a long one, or only what
+    items cost beside their tokens; rows of up to 80 parts."""
+    B, cache, q, cu, H = _case(dtype, dim, 64, 3, 1, qlens, klens, seed=26)
+    assert B.attention_cached_workspace_size(cache, cu, H, dtype) > 0
+    _check_attention(cache, q, _attend(B, cache, q, cu, H), cu, H, rows=12)

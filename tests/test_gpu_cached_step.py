@@ -5,6 +5,8 @@ A cached value is a code times a power of two, exact in bf16 and fp32, so
 dit_denoise_step on the cache's own values as a packed cache computes the same
 step; the two differ by the order of sums and roundings inside the
 cross-attention (the framework's tolerances for a step)."""
+import dataclasses
+
 import numpy as np
 import pytest
 import torch
@@ -25,7 +27,7 @@ def _i32(a):
 
 class CachedStep(DeviceStep):
     def __init__(self, name, page=32, rows=6, n_pages=40, width=8):
-        super().__init__(synth.get_model_workload(name))
+        super().__init__(synth.get_model_workload(name) if isinstance(name, str) else name)
         B, wl = self.B, self.mw.block
         self.page = page
         self.cache = B.KvCache.empty(n_pages, wl.n_heads, wl.head_dim, page, rows, width, n_blocks=self.n_blocks)
@@ -144,6 +146,22 @@ def test_prompts_of_length_zero_and_one(name):
     out = s.cached()
     assert torch.isfinite(out).all()
     s.agree(lens, f"{name} {lens}")
+
+
+@pytest.mark.parametrize("grids", [[(3, 4, 6), (1, 6, 10)], [(1, 4, 6), (1, 5, 6)]])
+@pytest.mark.parametrize("lens,width", [([77, 40], 4), ([2500, 700], 128)])
+def test_long_texts_and_small_latents(grids, lens, width):
+    """Requests of more and of fewer than 32 tokens, on texts whose tokens one
+    workgroup takes and on texts divided among workgroups."""
+    log(f"case cached step, latents {grids}, texts {lens}")
+    mw = synth.get_model_workload("step_small_bf16")
+    rows = tuple(f * h * w for f, h, w in grids)
+    mw = dataclasses.replace(mw, block=dataclasses.replace(mw.block, grids=tuple(grids), rows=rows))
+    s = CachedStep(mw, n_pages=120, width=width)
+    assert (s.B.attention_cached_workspace_size(s.cache, [0, *np.cumsum(rows)], mw.block.n_heads, torch.bfloat16) > 0) == (width > 4)
+    free = np.random.default_rng(5).permutation(120).tolist()
+    s.admit(_prompts(s, lens, 6), lens, free)
+    s.agree(lens, f"{grids} {lens}")
 
 
 @pytest.mark.parametrize("name", STEPS)
