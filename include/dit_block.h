@@ -412,8 +412,8 @@ dit_status dit_unpatchify_euler(const dit_model_config *cfg, const dit_varlen *v
  * on the host; no value in them makes a kernel leave its buffers.  A length
  * below 0 counts as 0, one over the table's width or the call's bound as that;
  * tokens on a page outside 0 .. n_pages - 1 are not there.  A page belongs to
- * one request: entries of one slot map that name a page twice leave either's
- * values in it. */
+ * one request: entries of one slot map that name a page twice leave that page's
+ * values undefined. */
 typedef struct {
   int n_blocks, n_pages, n_kv_heads;
   int head_dim;             /* 64 or 128 */
