@@ -379,6 +379,7 @@ template <int N> __device__ __forceinline__ void wait_vmcnt() { asm volatile("s_
 // ------------------------------------------------- bf16, many rows of a head
 
 constexpr float kHeadroom = 18446744073709551616.0f;   // 2^64, bound of a row sum
+constexpr float kFarScore = 4096.f;                    // bound of a row's reference
 
 // 4 waves of 32 rows, two workgroups per compute unit; tiles of 64 tokens (8 KB
 // of keys and 8 KB of values at 128 channels: half of bf16) in an LDS ring of 4,
@@ -386,8 +387,12 @@ constexpr float kHeadroom = 18446744073709551616.0f;   // 2^64, bound of a row s
 //
 // The row reference of the softmax is the first tile's row maximum for the
 // whole pass, so the loop neither searches maxima nor rescales the output.
-// Where a row's sum passes 2^64 the workgroup finds the exact maxima and runs
-// again, so the result is the softmax in any case.
+// The exponent is one multiply-add on the unrounded product, against a reference
+// that is rounded: all probabilities of a row carry the same factor 2^e, e at most
+// half a step of the reference.  Where that could matter (references past 2^12,
+// from where the parts of a row no longer agree to 2^-13) or a row's sum passes
+// 2^64, the workgroup finds the maxima of the rounded products and runs again on
+// these, the largest probability exactly 1.
 //
 // Bound by the matrix instructions at the clock that the power limit leaves:
 // 2,048 queries x 31,200 tokens x 32 heads of 128 take 832 us, 1.26 PFLOP/s.
@@ -477,7 +482,9 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
     split_row<HD, QNORM>(raw, fh, w, q);
     f32x16 oacc[ND];
     float l_run[2], m_ref = 0.f, x_max = -INFINITY;
-    bool have_ref = false;
+    // what a tile is for: the reference, the first pass against it, the maxima of
+    // the rounded products, the last pass against those
+    enum { kFirst, kAgainstFirst, kFindMax, kAgainstMax } phase = kFirst;
     const float c = w.scale_log2;
     const float off_score = c < 0.f ? INFINITY : -INFINITY;   // times c: -inf
 
@@ -496,8 +503,8 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       score_step<0, HD>(kf[0][0], kf[0][1], kf[1][0], kf[1][1], q, ks, s);
       if constexpr (NC == 2) score_step<1, HD>(kf[0][2], kf[0][3], kf[1][2], kf[1][3], q, ks, s);
     };
-    // P of the scores, and O += V P
-    auto output = [&](int t, const f32x16 (&s)[2]) __attribute__((always_inline)) {
+    // P of the scores (times c: log2 units), and O += V P
+    auto output = [&](int t, const f32x16 (&s)[2], float c) __attribute__((always_inline)) {
       bf16x8 p[4];
 #pragma unroll
       for (int hb = 0; hb < 2; ++hb)
@@ -526,7 +533,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       }
     };
 
-    auto run_pass = [&](bool track) __attribute__((always_inline)) {
+    auto run_pass = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int db = 0; db < ND; ++db) oacc[db] = f32x16{};
       l_run[0] = l_run[1] = 0.f;
@@ -546,7 +553,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
           if (t + 4 < c1) issue(t + 4);
         };
         for (int t = c0; t < c1;) {
-          if (!any_bad && have_ref && !track) {
+          if (!any_bad && phase == kAgainstFirst) {
             const int t_full = min(c1, len / 64);   // whole tiles
             for (; t < t_full; ++t) {
               // The older of two waves goes first wherever both could; with turns at a higher
@@ -559,7 +566,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
               if (row0 < rows) {
                 f32x16 s[2];
                 scores(t, s);
-                output(t, s);
+                output(t, s, c);
               }
               advance(t);
             }
@@ -594,15 +601,20 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
                   if (8 * (v >> 2) + 4 * fh + (v & 3) >= (hb ? n1 : n0)) s[hb][v] = off_score;
             }
             if (n0 + n1 > 0) {   // (nothing there: the reference waits for the next tile)
-              if (track || !have_ref) {
+              const float unit = phase >= kFindMax ? 1.f : c;
+              if (phase >= kFindMax) {
+                s[0] *= c;
+                s[1] *= c;
+              }
+              if (phase == kFirst || phase == kFindMax) {
                 float mx = -INFINITY;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, fmaxf(s[0][v] * c, s[1][v] * c));
-                if (track) x_max = fmaxf(x_max, mx);
+                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, fmaxf(s[0][v] * unit, s[1][v] * unit));
+                if (phase == kFindMax) x_max = fmaxf(x_max, mx);
                 else m_ref = pair_max<32>(mx);
-                have_ref = true;
               }
-              if (!track) output(t, s);
+              if (phase == kFirst) phase = kAgainstFirst;
+              if (phase != kFindMax) output(t, s, unit);
             }
           }
           advance(t);
@@ -611,23 +623,24 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       }
     };
 
-    // The first pass against the first tile's maxima; where a row sum passed 2^64
-    // (or overflowed), one to find the exact maxima and one against them.
     float l_tot;
 #pragma unroll 1
-    for (int pass = 0;; ++pass) {
-      run_pass(pass == 1);
-      if (pass == 1) {
+    for (;;) {
+      run_pass();
+      if (phase == kFindMax) {
         m_ref = pair_max<32>(x_max);
+        phase = kAgainstMax;
         continue;
       }
       l_tot = pair_sum<32>(l_run[0] + l_run[1]);
       if (tid == 0) s_redo = 0;
       __syncthreads();   // (and every wave has read its last tile: the ring is free)
-      if (pass == 2) break;
-      if (__builtin_amdgcn_ballot_w64(!(l_tot <= kHeadroom)) != 0 && lane == 0) s_redo = 1;
+      if (phase == kAgainstMax) break;
+      const bool fine = l_tot <= kHeadroom && fabsf(m_ref) <= kFarScore;
+      if (__builtin_amdgcn_ballot_w64(!fine) != 0 && lane == 0) s_redo = 1;
       __syncthreads();
       if (__builtin_amdgcn_readfirstlane(s_redo) == 0) break;
+      phase = kFindMax;
     }
 
     // oacc[db][4 i + j]: channel 32 db + 8 i + 4 fh + j of the lane's row
