@@ -380,6 +380,7 @@ template <int N> __device__ __forceinline__ void wait_vmcnt() { asm volatile("s_
 
 constexpr float kHeadroom = 18446744073709551616.0f;   // 2^64, bound of a row sum
 constexpr float kFarScore = 4096.f;                    // bound of a row's reference
+constexpr uint32_t kLargeScale = 127 + 48;             // bound of a value's scale byte: 2^64 * 448 * 2^48 is below 2^121
 
 // 4 waves of 32 rows, two workgroups per compute unit; tiles of 64 tokens (8 KB
 // of keys and 8 KB of values at 128 channels: half of bf16) in an LDS ring of 4,
@@ -390,8 +391,9 @@ constexpr float kFarScore = 4096.f;                    // bound of a row's refer
 // The exponent is one multiply-add on the unrounded product, against a reference
 // that is rounded: all probabilities of a row carry the same factor 2^e, e at most
 // half a step of the reference.  Where that could matter (references past 2^12,
-// from where the parts of a row no longer agree to 2^-13) or a row's sum passes
-// 2^64, the workgroup finds the maxima of the rounded products and runs again on
+// from where the parts of a row no longer agree to 2^-13), a row's sum passes 2^64
+// or values are so large that a product with a probability of 2^64 could pass
+// fp32, the workgroup finds the maxima of the rounded products and runs again on
 // these, the largest probability exactly 1.
 //
 // Bound by the matrix instructions at the clock that the power limit leaves:
@@ -482,6 +484,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
     split_row<HD, QNORM>(raw, fh, w, q);
     f32x16 oacc[ND];
     float l_run[2], m_ref = 0.f, x_max = -INFINITY;
+    bool large = false;   // some page of the tokens has values past kLargeScale
     // what a tile is for: the reference, the first pass against it, the maxima of
     // the rounded products, the last pass against those
     enum { kFirst, kAgainstFirst, kFindMax, kAgainstMax } phase = kFirst;
@@ -543,6 +546,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
         begun = false;
         wait_vmcnt<0>();   // the first tiles, asked for with the queries and scales; only tile loads are counted from here on
         __syncthreads();
+        large |= __builtin_amdgcn_ballot_w64((scales >> 8 & 0xFFu) > kLargeScale || scales >> 24 > kLargeScale) != 0;
         // tile t is done: tile t + 1 in LDS for every wave; tile t + 4 into the slot of t
         auto advance = [&](int t) __attribute__((always_inline)) {
           if (t + 1 >= c1) return;
@@ -636,7 +640,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       if (tid == 0) s_redo = 0;
       __syncthreads();   // (and every wave has read its last tile: the ring is free)
       if (phase == kAgainstMax) break;
-      const bool fine = l_tot <= kHeadroom && fabsf(m_ref) <= kFarScore;
+      const bool fine = l_tot <= kHeadroom && fabsf(m_ref) <= kFarScore && !large;
       if (__builtin_amdgcn_ballot_w64(!fine) != 0 && lane == 0) s_redo = 1;
       __syncthreads();
       if (__builtin_amdgcn_readfirstlane(s_redo) == 0) break;

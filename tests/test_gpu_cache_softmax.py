@@ -1,5 +1,6 @@
 """The cached attention's softmax where its references and sums leave the
-ordinary range: scores of 2^33."""
+ordinary range: scores of 2^33, values whose products with an unfinished
+probability pass fp32."""
 import numpy as np
 import pytest
 import torch
@@ -12,6 +13,26 @@ pytestmark = pytest.mark.gpu
 # one short request in whole items or one long one in shares of its tokens, for the
 # kernel of few rows (20) and that of many (300)
 SIZES = [(20, 200), (300, 200), (20, 5000), (300, 5000)]
+
+
+def _pages(B, k, v, ks, vs, page=32):
+    """A cache of one request and head with these codes [tokens, channels] and scale bytes per page."""
+    n, d = k.shape
+    m = -(-n // page)
+    c = B.KvCache.empty(m, 1, d, page, 1, m)
+    for pool, codes, place in ((c.k, k, C.k_place), (c.v, v, C.v_place)):
+        x = np.full(tuple(pool.shape[3:]), 0x7F, np.uint8)
+        x = np.broadcast_to(x, (m,) + x.shape).copy()
+        for p in range(m):
+            rows = codes[p * page:(p + 1) * page]
+            t, ch = np.meshgrid(np.arange(len(rows)), np.arange(d), indexing="ij")
+            x[p][place(t, ch)] = rows
+        pool[0, :, 0] = torch.from_numpy(x).cuda()
+    c.k_scale[0, :, 0] = torch.from_numpy(np.asarray(ks, np.uint8)).cuda()
+    c.v_scale[0, :, 0] = torch.from_numpy(np.asarray(vs, np.uint8)).cuda()
+    c.table.copy_(torch.arange(m, dtype=torch.int32).view(1, m))
+    c.lens.fill_(n)
+    return c
 
 
 def _tokens(cache, n):
@@ -52,3 +73,26 @@ def test_scores_of_any_size(dtype, dim, rows, tokens, octave):
     half = BF16_HALF if dtype == BF16 else 2.0 ** -20
     bad = (np.abs(got - want)[clear] > 2 * half * np.abs(want)[clear] + 1e-8).any(1)
     assert not bad.any(), f"{bad.sum()} of {len(bad)} rows"
+
+
+@pytest.mark.parametrize("dtype,dim", TYPES)
+@pytest.mark.parametrize("rows,tokens", SIZES)
+@pytest.mark.parametrize("byte,code", [(197, 1.5), (175, 448.0), (176, -448.0), (247, -192.0)])
+def test_large_values(dtype, dim, rows, tokens, byte, code):
+    """One token's score lies 60 octaves over the others', below the 2^64 at which
+    a row's sum alone would show it, and its value times 2^60 passes fp32."""
+    B = require_gpu()
+    log(f"case value {code} x 2^{byte - 127} {dtype} dim {dim} rows {rows} tokens {tokens}")
+    m, far = -(-tokens // 32), tokens - 70
+    k, v = np.zeros((tokens, dim), np.uint8), np.zeros((tokens, dim), np.uint8)
+    k[far, 0] = C.codes(60.0)
+    v[far] = C.codes(code * (1 - 0.5 * (np.arange(dim) % 2)))   # the code and half of it in turn
+    vs = np.full(m, 120)
+    vs[far // 32] = byte
+    cache = _pages(B, k, v, np.full(m, 127), vs)
+    q, _ = _bits(np.eye(1, dim).repeat(rows, 0), dtype)
+    o = _attend(B, cache, q, [0, rows], 1, float(np.log(2)))   # a score of 60 is 2^60
+    got = o.double().cpu().numpy()
+    want = C.VALUES[v[far]] * 2.0 ** (byte - 127)
+    half = BF16_HALF if dtype == BF16 else 2.0 ** -20
+    assert (np.abs(got - want) <= 2 * half * np.abs(want)).all(), (got[0, :2], want[:2])
