@@ -633,6 +633,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
       run_pass();
       if (phase == kFindMax) {
         m_ref = pair_max<32>(x_max);
+        if (m_ref == -INFINITY) m_ref = 0.f;   // scores of -inf only: probabilities of 0
         phase = kAgainstMax;
         continue;
       }
@@ -819,17 +820,18 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __
       mx = pair_max<32>(mx);
       if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
         const float m_new = fmaxf(m, mx);
-        const float a = __builtin_amdgcn_exp2f(m - m_new);   // the first group: 2^-inf = 0
+        const float a = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.f : m_new));   // the first group: 2^-inf = 0
         m = m_new;
         l *= a;
 #pragma unroll
         for (int d = 0; d < ND; ++d) oacc[d] *= a;
       }
+      const float ref = m == -INFINITY ? 0.f : m;   // scores of -inf only so far
       bf16x8 p[2];
       float lp[2] = {0.f, 0.f};
 #pragma unroll
       for (int v = 0; v < 16; v += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(s[v] - m), p1 = __builtin_amdgcn_exp2f(s[v + 1] - m);
+        const float p0 = __builtin_amdgcn_exp2f(s[v] - ref), p1 = __builtin_amdgcn_exp2f(s[v + 1] - ref);
         const bf16x2 pr = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
         p[v >> 3][v & 7] = pr[0];
         p[v >> 3][(v & 7) + 1] = pr[1];

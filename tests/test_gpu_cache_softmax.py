@@ -1,6 +1,6 @@
 """The cached attention's softmax where its references and sums leave the
 ordinary range: scores of 2^33, values whose products with an unfinished
-probability pass fp32."""
+probability pass fp32, scores of minus infinity."""
 import numpy as np
 import pytest
 import torch
@@ -96,3 +96,31 @@ def test_large_values(dtype, dim, rows, tokens, byte, code):
     want = C.VALUES[v[far]] * 2.0 ** (byte - 127)
     half = BF16_HALF if dtype == BF16 else 2.0 ** -20
     assert (np.abs(got - want) <= 2 * half * np.abs(want)).all(), (got[0, :2], want[:2])
+
+
+@pytest.mark.parametrize("dtype,dim", TYPES)
+@pytest.mark.parametrize("rows,tokens", SIZES)
+@pytest.mark.parametrize("where", ["first", "last"])
+def test_scores_of_minus_infinity(dtype, dim, rows, tokens, where):
+    """Tokens whose score is below fp32's range have no weight, in front of the
+    others or behind them, in some rows of a call and not in others."""
+    B = require_gpu()
+    log(f"case scores of minus infinity {where} {dtype} dim {dim} rows {rows} tokens {tokens}")
+    rng = np.random.default_rng(3)
+    m, n = -(-tokens // 32), tokens // 2 // 32 * 32
+    k = np.zeros((tokens, dim), np.uint8)
+    low = np.arange(tokens) < n if where == "first" else np.arange(tokens) >= n
+    k[low, 0] = C.codes(32.0)
+    v = C.codes(rng.standard_normal((tokens, dim)))
+    cache = _pages(B, k, v, np.full(m, 152), np.full(m, 127))   # 2^5 * 2^25
+    x = np.zeros((rows, dim))
+    x[:, 0] = np.where(np.arange(rows) % 3, -2.0 ** 100, 0.0)   # powers of two: the whole product overflows, not a part of it
+    q, _ = _bits(x, dtype)
+    got = _attend(B, cache, q, [0, rows], 1).double().cpu().numpy()
+    V = C.VALUES[v]
+    for r in range(rows):
+        use = V[~low] if r % 3 else V
+        want = use.mean(0)
+        # equal scores: bf16 probabilities of exactly 1, fp32 sums of the values, the result's rounding
+        tol = (BF16_HALF if dtype == BF16 else 2.0 ** -23) * np.abs(want) + (len(use) + 16) * 2.0 ** -24 * np.abs(use).mean(0)
+        assert (np.abs(got[r] - want) <= tol).all(), (r, got[r, :3], want[:3])
