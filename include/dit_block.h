@@ -413,7 +413,8 @@ dit_status dit_unpatchify_euler(const dit_model_config *cfg, const dit_varlen *v
  * below 0 counts as 0, one over the table's width or the call's bound as that;
  * tokens on a page outside 0 .. n_pages - 1 are not there.  A page belongs to
  * one request: entries of one slot map that name a page twice leave that page's
- * values undefined. */
+ * values undefined.  So does whatever is written while a call reads it: a table
+ * or length that changes meanwhile leaves that call's results undefined. */
 typedef struct {
   int n_blocks, n_pages, n_kv_heads;
   int head_dim;             /* 64 or 128 */

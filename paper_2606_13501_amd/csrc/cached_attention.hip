@@ -72,25 +72,31 @@ struct CachedWork {
 
 // The request's cached length, within the table and the caller's bound.
 __device__ __forceinline__ int length_of(const CachedWork& w, int r) { return min(max(w.lens[r], 0), w.max_len); }
-__device__ __forceinline__ int units_of(const CachedWork& w, int r) {
-  return (length_of(w, r) + (1 << w.unit_shift) - 1) >> w.unit_shift;
-}
+__device__ __forceinline__ int units_of(const CachedWork& w, int len) { return (len + (1 << w.unit_shift) - 1) >> w.unit_shift; }
 
 // What an item of the request costs, in units; one without tokens is left to
 // cached_attn_merge.
 __device__ __forceinline__ int cost_of(const CachedWork& w, int units) { return units > 0 ? units + w.extra : 0; }
 
-// ends[i] = cost of requests 0 .. i; by the first wave, for the workgroup.
-__device__ __forceinline__ void count_units(const CachedWork& w, int64_t* ends) {
+// The requests' lengths, read once, and what their items cost; by the first wave,
+// for the workgroup.  Nothing reads a length again: a length that is written
+// meanwhile gives a wrong row, but no item outside its request.
+struct Counted {
+  int64_t ends[kWave];   // cost of requests 0 .. i
+  int len[kWave];
+};
+__device__ __forceinline__ void count_units(const CachedWork& w, Counted& c) {
   if (threadIdx.x < kWave) {
     const int i = threadIdx.x;
-    int64_t v = i < w.n_req ? (int64_t)w.tiles[i] * w.n_kv_heads * cost_of(w, units_of(w, w.req[i])) : 0;
+    const int len = i < w.n_req ? length_of(w, w.req[i]) : 0;
+    int64_t v = i < w.n_req ? (int64_t)w.tiles[i] * w.n_kv_heads * cost_of(w, units_of(w, len)) : 0;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
       const int64_t below = __shfl_up(v, o, kWave);
       if (i >= o) v += below;
     }
-    ends[i] = v;
+    c.ends[i] = v;
+    c.len[i] = len;
   }
   __syncthreads();
 }
@@ -107,6 +113,7 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
 // A workgroup's next piece of work: units u0 .. u1 of an item's tokens.
 struct Segment {
   int i, head, tile;   // position in the work table, key/value head, row tile
+  int len;             // the request's cached length
   int u0, u1;
   int slot;            // where its unfinished rows go (-1: it has all of the item's tokens)
 };
@@ -130,6 +137,7 @@ __device__ __forceinline__ bool whole_item(const CachedWork& w, Segment& g) {
   int item;
   g.i = 0;
   if (w.n_req == 1) {   // without waiting for a length
+    g.len = length_of(w, w.req[0]);
     const int lo = xcd * w.prefix[1] / kXcds;   // (kMaxItems * 8 fits)
     item = lo + at;
     if (item >= (xcd + 1) * w.prefix[1] / kXcds) return false;
@@ -146,11 +154,13 @@ __device__ __forceinline__ bool whole_item(const CachedWork& w, Segment& g) {
     if (here == 0) return false;
     g.i = __builtin_ctzll(here);
     item = __builtin_amdgcn_readlane(lo + at - start, g.i);
+    g.len = __builtin_amdgcn_readlane(len, g.i);
   }
   g.head = item / w.tiles[g.i];
   g.tile = item - g.head * w.tiles[g.i];
   g.u0 = 0;
-  g.u1 = __builtin_amdgcn_readfirstlane(units_of(w, w.req[g.i]));
+  g.len = __builtin_amdgcn_readfirstlane(g.len);
+  g.u1 = units_of(w, g.len);
   g.slot = -1;
   return true;
 }
@@ -172,24 +182,25 @@ struct Share {
   int s;
   int64_t pos, end;
 };
-__device__ __forceinline__ Share my_share(const CachedWork& w, int64_t* ends) {
-  count_units(w, ends);
-  const int64_t all = uniform(ends[kWave - 1]), share = uniform(share_of(w, all));
+__device__ __forceinline__ Share my_share(const CachedWork& w, Counted& c) {
+  count_units(w, c);
+  const int64_t all = uniform(c.ends[kWave - 1]), share = uniform(share_of(w, all));
   Share x;
   x.s = (blockIdx.x % kXcds) * (w.shares / kXcds) + blockIdx.x / kXcds;
   x.pos = x.s * share;
   x.end = min(x.pos + share, all);
   return x;
 }
-__device__ __forceinline__ bool next_segment(const CachedWork& w, const int64_t* ends, Share& x, Segment& g) {
+__device__ __forceinline__ bool next_segment(const CachedWork& w, const Counted& c, Share& x, Segment& g) {
   while (x.pos < x.end) {
-    int64_t start = 0, upto = uniform(ends[0]);
+    int64_t start = 0, upto = uniform(c.ends[0]);
     int r = 0;
     while (upto < x.end) {
       start = upto;
-      upto = uniform(ends[++r]);
+      upto = uniform(c.ends[++r]);
     }
-    const int units = __builtin_amdgcn_readfirstlane(units_of(w, w.req[r]));
+    g.len = __builtin_amdgcn_readfirstlane(c.len[r]);
+    const int units = units_of(w, g.len);
     const int cost = cost_of(w, units);
     const int64_t item = uniform((x.end - 1 - start) / cost);
     const int64_t begin = start + item * cost;
@@ -416,15 +427,19 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
   constexpr int kRing = 4;
   __shared__ __attribute__((aligned(1024))) char smem[kRing * kSlot];
   __shared__ int s_redo;
-  __shared__ int64_t ends[SHARES ? kWave : 1];
+  __shared__ std::conditional_t<SHARES, Counted, int> counted;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int fr = lane & 31, fh = lane >> 5;
   Segment it;
   Share share{};
+  auto more = [&]() __attribute__((always_inline)) {
+    if constexpr (SHARES) return next_segment(w, counted, share, it);
+    else return false;
+  };
   if constexpr (SHARES) {
-    share = my_share(w, ends);
-    if (!next_segment(w, ends, share, it)) return;
+    share = my_share(w, counted);
+    if (!more()) return;
   } else {
     if (!whole_item(w, it)) return;
   }
@@ -432,7 +447,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
     const int r = w.req[it.i];
     const int rows = w.q_len[it.i] * w.group;
     const int row0 = it.tile * 128 + wave * 32;   // this wave's rows: row0 ..
-    const int len = __builtin_amdgcn_readfirstlane(length_of(w, r));
+    const int len = it.len;
     const int t_begin = it.u0, t_end = it.u1;   // tiles: units of 64 tokens
 
     const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_char*)smem;
@@ -686,7 +701,7 @@ __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restric
         *reinterpret_cast<u32x4*>(O + query_at(w, it, row, w.o_stride, HD) + 8 * i) = x;
     }
     __builtin_amdgcn_wave_barrier();
-  } while (SHARES && next_segment(w, ends, share, it));
+  } while (more());
 }
 
 // ------------------------------------------------ the waves' shares, joined
@@ -746,15 +761,19 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __
   constexpr int NC = HD / 64, ND = HD / 32, kGroup = 32 * HD, WAVES = kKeyWaves;
   __shared__ __attribute__((aligned(16))) float part_o[WAVES][32][HD + 4];
   __shared__ float part_m[WAVES][32], part_l[WAVES][32];
-  __shared__ int64_t ends[SHARES ? kWave : 1];
+  __shared__ std::conditional_t<SHARES, Counted, int> counted;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int fr = lane & 31, fh = lane >> 5;
   Segment it;
   Share share{};
+  auto more = [&]() __attribute__((always_inline)) {
+    if constexpr (SHARES) return next_segment(w, counted, share, it);
+    else return false;
+  };
   if constexpr (SHARES) {
-    share = my_share(w, ends);
-    if (!next_segment(w, ends, share, it)) return;
+    share = my_share(w, counted);
+    if (!more()) return;
   } else {
     if (!whole_item(w, it)) return;
   }
@@ -762,7 +781,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __
     const int r = w.req[it.i];
     const int rows = w.q_len[it.i] * w.group;
     const int row = min(fr, rows - 1);
-    const int len = __builtin_amdgcn_readfirstlane(length_of(w, r));
+    const int len = it.len;
     const int g_begin = 4 * it.u0, g_end = min(4 * it.u1, (len + 31) / 32);   // units of 128 tokens
     const int n_mine = max(0, (g_end - g_begin - wave + WAVES - 1) / WAVES);   // groups g_begin + wave + WAVES i
 
@@ -883,7 +902,7 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __
             f32x4{oacc[d][4 * i], oacc[d][4 * i + 1], oacc[d][4 * i + 2], oacc[d][4 * i + 3]};
     __syncthreads();
     join_waves<HD, 32, WAVES>(part_o, part_m, part_l, 0, rows, it, w, O);
-  } while (SHARES && next_segment(w, ends, share, it));
+  } while (more());
 }
 
 // ------------------------------------------------------------------- fp32
@@ -904,15 +923,19 @@ __global__ __launch_bounds__(64 * kKeyWaves, SHARES ? 2 : 4) void cached_attn_f3
   constexpr int NB = HD / 16, kGroup = 32 * HD, WAVES = kKeyWaves;
   __shared__ __attribute__((aligned(16))) float part_o[WAVES][16][HD + 4];
   __shared__ float part_m[WAVES][16], part_l[WAVES][16];
-  __shared__ int64_t ends[SHARES ? kWave : 1];
+  __shared__ std::conditional_t<SHARES, Counted, int> counted;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g4 = lane >> 4;
   Segment it;
   Share share{};
+  auto more = [&]() __attribute__((always_inline)) {
+    if constexpr (SHARES) return next_segment(w, counted, share, it);
+    else return false;
+  };
   if constexpr (SHARES) {
-    share = my_share(w, ends);
-    if (!next_segment(w, ends, share, it)) return;
+    share = my_share(w, counted);
+    if (!more()) return;
   } else {
     if (!whole_item(w, it)) return;
   }
@@ -920,7 +943,7 @@ __global__ __launch_bounds__(64 * kKeyWaves, SHARES ? 2 : 4) void cached_attn_f3
     const int req = w.req[it.i];
     const int rows = w.q_len[it.i] * w.group;
     const int row = min(it.tile * 16 + r, rows - 1);
-    const int len = __builtin_amdgcn_readfirstlane(length_of(w, req));
+    const int len = it.len;
     const int t_begin = 8 * it.u0, t_end = min(8 * it.u1, (len + 15) / 16);   // units of 128 tokens
     const int n_mine = max(0, (t_end - t_begin - wave + WAVES - 1) / WAVES);   // tiles t_begin + wave + WAVES i
     uint32_t at = kNoGroup, scales = 0;   // lane i: the group of this wave's tile base + i
@@ -1021,7 +1044,7 @@ __global__ __launch_bounds__(64 * kKeyWaves, SHARES ? 2 : 4) void cached_attn_f3
     for (int c = 0; c < NB; ++c) *reinterpret_cast<f32x4*>(&part_o[wave][r][16 * c + 4 * g4]) = acc[c];
     __syncthreads();
     join_waves<HD, 16, WAVES>(part_o, part_m, part_l, it.tile * 16, rows, it, w, O);
-  } while (SHARES && next_segment(w, ends, share, it));
+  } while (more());
 }
 
 // The rows whose tokens lay in several shares, joined in the shares' order: O =
@@ -1048,9 +1071,9 @@ __device__ __forceinline__ void join(Joined& x, float top, float l, f32x4 o) {
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void cached_attn_merge(T* __restrict__ O, CachedWork w) {
   constexpr int LANES = HD / 4, GROUPS = 256 / LANES;   // lanes of a row, rows at a time
-  __shared__ int64_t ends[kWave];
+  __shared__ Counted counted;
   __shared__ Joined halves[GROUPS][LANES];
-  count_units(w, ends);
+  count_units(w, counted);
   const int per_item = w.tile_rows / w.merge_rows;
   const int item = blockIdx.x / per_item, at0 = blockIdx.x % per_item * w.merge_rows;
   const int lane = threadIdx.x % kWave, group = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
@@ -1059,11 +1082,11 @@ __global__ __launch_bounds__(256) void cached_attn_merge(T* __restrict__ O, Cach
   const int nth = item - w.prefix[it.i];
   it.head = nth / w.tiles[it.i];
   it.tile = nth - it.head * w.tiles[it.i];
-  const int units = __builtin_amdgcn_readfirstlane(units_of(w, w.req[it.i]));
+  const int units = __builtin_amdgcn_readfirstlane(units_of(w, counted.len[it.i]));
   int s0 = 0, s1 = -1;
   if (units > 0) {
-    const int64_t first = uniform((it.i > 0 ? ends[it.i - 1] : 0) + (int64_t)nth * cost_of(w, units) + w.extra);
-    const int64_t share = uniform(share_of(w, ends[kWave - 1]));
+    const int64_t first = uniform((it.i > 0 ? counted.ends[it.i - 1] : 0) + (int64_t)nth * cost_of(w, units) + w.extra);
+    const int64_t share = uniform(share_of(w, counted.ends[kWave - 1]));
     s0 = (int)(first / share);
     s1 = (int)((first + units - 1) / share);
     if (s0 == s1) return;   // written by its workgroup
