@@ -461,7 +461,8 @@ dit_status dit_cache_tables(const dit_kv_cache *cache, int n_req, const int32_t 
  * finite value of its tokens exceeds 448 * 2^e; an entry that continues a page
  * leaves the scale or makes it larger, and then brings the page's earlier codes
  * to it.  Codes are rounded to nearest, ties to even; infinities become NaN.
- * Places behind the entry's tokens and all other pages keep their bytes. */
+ * Places behind the entry's tokens and all other pages keep their bytes.  Without
+ * rows (n_rows 0, k and v may be NULL) nothing is written. */
 dit_status dit_cache_store(const dit_kv_cache *cache, int block, const void *k, const void *v,
                            int64_t k_row_stride, int64_t v_row_stride, int64_t n_rows,
                            const int32_t *runs, int n_runs, dit_dtype dtype, hipStream_t stream);
@@ -472,7 +473,8 @@ dit_status dit_cache_store(const dit_kv_cache *cache, int block, const void *k, 
  * query head h on key/value head h / (n_heads / n_kv_heads).  q, o, strides and
  * softmax_scale as for dit_attention_varlen; head_dim (64 or 128 in both
  * dtypes) and n_kv_heads, a divisor of n_heads, are the cache's.  A request
- * without tokens gets rows of zeros; table rows from n_req on are not read.
+ * without tokens gets rows of zeros; table rows from n_req on are not read.  A
+ * batch without query rows does nothing (q and o may be NULL).
  * max_len bounds the lengths (0: the table's width): longer requests are cut
  * there, and the work is divided by it.  Where whole row tiles would leave
  * compute units idle, the tokens are divided among the workgroups and what
@@ -491,7 +493,8 @@ dit_status dit_attention_cached(const dit_kv_cache *cache, int block, const void
  * rows that runs names go to their places in every block's pages (from
  * dit_cache_tables with n_rows = vl->cu_seqlens_txt[n_req]).  The workspace
  * holds one block's keys and values in the config's dtype,
- * dit_text_kv_cached_workspace_size bytes, 256-byte aligned. */
+ * dit_text_kv_cached_workspace_size bytes, 256-byte aligned.  Prompts without
+ * rows: nothing is done, and txt and ws may be NULL. */
 size_t dit_text_kv_cached_workspace_size(const dit_model_config *cfg, const dit_varlen *vl);
 dit_status dit_text_kv_cached(const dit_model_config *cfg, const dit_model_weights *w,
                               const dit_varlen *vl, const void *txt, const dit_kv_cache *cache,

@@ -603,11 +603,12 @@ def text_kv_cached_workspace_size(cfg: ModelConfig, vl: Varlen) -> int:
 
 
 def text_kv_cached(cfg: ModelConfig, w: ModelWeights, vl: Varlen, txt, cache: KvCache, runs, ws, stream=None):
+    """ws: as text_kv_cached_workspace_size says (None for prompts without rows)."""
     _want(runs, "runs", torch.int32, (runs.shape[0], 4))
     s = _cache_stream(cache, stream, txt, runs, ws)
     _check(lib().dit_text_kv_cached(ctypes.byref(cfg.c), ctypes.byref(w.c), ctypes.byref(vl.c), txt.data_ptr(), cache.ref,
-                                    runs.data_ptr(), runs.shape[0], ws.data_ptr(), ws.numel() * ws.element_size(), s),
-           "dit_text_kv_cached")
+                                    runs.data_ptr(), runs.shape[0], _at(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+                                    s), "dit_text_kv_cached")
 
 
 def denoise_cached_workspace_size(cfg: ModelConfig, vl: Varlen, cache: KvCache) -> int:

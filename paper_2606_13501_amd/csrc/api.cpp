@@ -1276,7 +1276,7 @@ dit_status dit_cache_store(const dit_kv_cache* cache, int block, const void* k, 
   DIT_TRY(check_dtype(dtype));
   DIT_TRY(check_cache(cache, true, 0));
   DIT_TRY(check_cache_block(cache, block));
-  DIT_TRY(check_ptr(k, "k")); DIT_TRY(check_ptr(v, "v"));
+  DIT_TRY(check_ptr(k, "k", n_rows == 0)); DIT_TRY(check_ptr(v, "v", n_rows == 0));   // (an empty tensor's address is 0)
   if (n_rows < 0 || n_rows > 0x7FFFFFFF) return fail(DIT_ERR_INVALID_ARG, "n_rows %lld", (long long)n_rows);
   if (n_runs < 0) return fail(DIT_ERR_INVALID_ARG, "slot map of %d entries", n_runs);
   DIT_TRY(check_ptr(runs, "runs", n_runs == 0));
@@ -1297,6 +1297,7 @@ dit_status dit_cache_store(const dit_kv_cache* cache, int block, const void* k, 
   for (int i = 0; i < 4; ++i)
     for (int j = i + 1; j < 7; ++j)
       if (overlaps(out[i], j < 4 ? out[j] : in[j - 4])) return fail(DIT_ERR_INVALID_ARG, "%s overlaps %s", names[i], names[j]);
+  if (n_rows == 0) return DIT_OK;
   return run_cache_store(cache, block, k, v, k_row_stride, v_row_stride, n_rows, runs, n_runs, dtype, stream);
 }
 
@@ -1318,7 +1319,7 @@ dit_status dit_attention_cached(const dit_kv_cache* cache, int block, const void
   DIT_TRY(check_cache(cache, true, n_req));
   DIT_TRY(check_cache_block(cache, block));
   DIT_TRY(check_cached_heads(cache, n_heads));
-  DIT_TRY(check_ptr(q, "q")); DIT_TRY(check_ptr(o, "o"));
+  DIT_TRY(check_ptr(q, "q", cu_q[n_req] == 0)); DIT_TRY(check_ptr(o, "o", cu_q[n_req] == 0));
   if (max_len < 0) return fail(DIT_ERR_INVALID_ARG, "max_len = %d", max_len);
   if (!isfinite(softmax_scale)) return fail(DIT_ERR_INVALID_ARG, "softmax_scale is not finite");
   const float scale = softmax_scale == 0.f ? 1.0f / sqrtf((float)cache->head_dim) : softmax_scale;
@@ -1362,7 +1363,7 @@ dit_status dit_text_kv_cached(const dit_model_config* cfg, const dit_model_weigh
   DIT_TRY(check_varlen(vl, true));
   DIT_TRY(check_text_weights(cfg, w));
   DIT_TRY(check_model_cache(cfg, cache, 0));
-  DIT_TRY(check_ptr(txt, "txt"));
+  DIT_TRY(check_ptr(txt, "txt", vl->cu_seqlens_txt[vl->n_req] == 0));
   if (n_runs < 0 || (int64_t)n_runs * 2 * cache->n_kv_heads > 0x7FFFFFFF) return fail(DIT_ERR_INVALID_ARG, "slot map of %d entries", n_runs);
   DIT_TRY(check_ptr(runs, "runs", n_runs == 0));
   const size_t need = dit_text_kv_cached_workspace_size(cfg, vl);
