@@ -300,7 +300,7 @@ hipError_t store_page(const CacheStoreArgs& p, dim3 grid, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_cache_tables(const CacheTablesArgs& p, hipStream_t s) {
-  const int blocks = p.n_runs > 0 ? (p.n_runs + 255) / 256 : 1;
+  const int blocks = p.n_runs > 0 ? (p.n_runs - 1) / 256 + 1 : 1;   // (n_runs + 255 may pass 32 bits)
   cache_tables_kernel<<<blocks, 256, 0, s>>>(p);
   return hipGetLastError();
 }
