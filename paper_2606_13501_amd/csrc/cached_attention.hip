@@ -14,8 +14,8 @@
 // S^T = K Q^T in bf16.  The keys' codes go to v_mfma_scale_f32_32x32x64_f8f6f4
 // as they are stored, with the page's scale byte as the instruction's block
 // scale.  A bf16 query value has 8 significant bits, two e4m3 values 4 each:
-// q = q1 + q2 exactly (values below 2^-15 of the largest of their 64 channels
-// to 2^-23 of it), so two of the fp8 instructions, at twice the bf16 rate,
+// q = q1 + q2 exactly (values below 2^-13.8 of the largest of their 64 channels
+// to 2^-21.8 of it), so two of the fp8 instructions, at twice the bf16 rate,
 // give what a bf16 product of converted keys would, without the conversion.
 // O^T = V^T P^T in bf16 MFMAs: v_cvt_scalef32_pk_bf16_fp8 turns two codes into
 // bf16 with the page's scale, exactly.
