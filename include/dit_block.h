@@ -397,8 +397,9 @@ dit_status dit_unpatchify_euler(const dit_model_config *cfg, const dit_varlen *v
  *
  * A value is a float8 e4m3 code (4 significant bits, largest 448) times a power
  * of two, 2^(s - 127), with one scale byte s for each page and head, in
- * k_scale / v_scale [n_blocks, n_pages, n_kv_heads].  The tokens of a page lie
- * in groups of 32, in the order in which a matrix instruction takes them:
+ * k_scale / v_scale [n_blocks, n_pages, n_kv_heads].  dit_cache_store writes s
+ * from 27 to 247; pages that a caller fills keep to that range.  The tokens of a
+ * page lie in groups of 32, in the order in which a matrix instruction takes them:
  *   k [n_blocks, n_pages, n_kv_heads, page_tokens / 32, head_dim / 16, 32, 16]:
  *     element (.., g, c, t, e) is token 32 g + t, channel 16 c + e;
  *   v [n_blocks, n_pages, n_kv_heads, page_tokens / 32, 2, head_dim, 16]:
@@ -475,6 +476,9 @@ dit_status dit_cache_store(const dit_kv_cache *cache, int block, const void *k, 
  * dtypes) and n_kv_heads, a divisor of n_heads, are the cache's.  A request
  * without tokens gets rows of zeros; table rows from n_req on are not read.  A
  * batch without query rows does nothing (q and o may be NULL).
+ * Scores, probabilities' sums and products are fp32: a score of minus infinity
+ * has no weight (a row of nothing else is zeros), one of infinity gives NaN, and
+ * a row's sum of |v| over its tokens has to stay in range.
  * max_len bounds the lengths (0: the table's width): longer requests are cut
  * there, and the work is divided by it.  Where whole row tiles would leave
  * compute units idle, the tokens are divided among the workgroups and what
@@ -504,7 +508,8 @@ dit_status dit_text_kv_cached(const dit_model_config *cfg, const dit_model_weigh
 /* dit_denoise_step with the text keys and values of a cache: request r of the
  * batch attends to row r of the cache's table.  vl->cu_seqlens_txt is not read
  * and may be NULL.  A captured step may be replayed for other prompts: the
- * table and lens name them. */
+ * table and lens name them.  The cross-attention's work is divided by the table's
+ * width, so a table for prompts is best as wide as the longest of them. */
 size_t dit_denoise_cached_workspace_size(const dit_model_config *cfg, const dit_varlen *vl,
                                          const dit_kv_cache *cache);
 dit_status dit_denoise_step_cached(const dit_model_config *cfg, const dit_model_weights *w,

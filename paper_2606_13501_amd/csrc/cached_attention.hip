@@ -24,8 +24,8 @@
 // the multiply-add that takes off the row's reference.  (Multiplied into the
 // query instead, it would have to be rounded to bf16 with it: the output was
 // then 0.0037 off the exact one, root mean square, 0.0017 of which is its own
-// rounding; now 0.0024.)  Probabilities are rounded to bf16, 8 significant bits
-// each.
+// rounding; now 0.0023.)  Probabilities are rounded to bf16, 8 significant bits
+// each: the rest of the 0.0023.
 #include <float.h>
 
 #include <algorithm>
@@ -415,7 +415,8 @@ constexpr uint32_t kLargeScale = 127 + 48;             // bound of a value's sca
 // among this one's softmax, or 50% at 2.0 GHz, 64 rows per wave and one
 // workgroup per compute unit, and took as long or longer.)  Short prompts: the
 // first tokens and rows are waited for most of half the time; 32,760 queries x
-// 512 tokens x 40 heads of 128 take 388 us, 0.89 PFLOP/s and 1.7 TB/s.
+// 512 tokens x 40 heads of 128 take 388 us, 0.89 PFLOP/s and 1.7 TB/s (and 414 on
+// a card that held 1.89 GHz meanwhile; five images on 18 to 512 tokens ran at 2.17).
 template <int HD, bool QNORM, bool SHARES>
 __global__ __launch_bounds__(256, 2) void cached_attn_many(const bf16* __restrict__ Q, bf16* __restrict__ O,
                                                            CachedWork w) {
@@ -915,8 +916,9 @@ __global__ __launch_bounds__(64 * kKeyWaves) void cached_attn_few(const bf16* __
 // sizes (64 queries x 77 tokens x 6 heads of 64: 7.5 us): the next tile is asked
 // for before the last is computed.  With many items the fp32 matrix rate is what
 // is left (400 x 512 tokens x 40 heads of 128: 59 us, 30 us of it in matrix
-// instructions); two workgroups per compute unit, at the price of two spilled
-// registers, took it there from 87.
+// instructions); two workgroups of whole items per compute unit, at the price of
+// two spilled registers, took it there from 87 (in shares, whose kernel needs 148
+// registers at 128 channels, one fits).
 template <int HD, bool SHARES>
 __global__ __launch_bounds__(64 * kKeyWaves, SHARES ? 2 : 4) void cached_attn_f32(const float* __restrict__ Q, float* __restrict__ O,
                                                                   CachedWork w) {
@@ -1140,7 +1142,6 @@ constexpr int64_t kMaxItems = (1 << 22);   // 512 threads each: a launch of fewe
 
 enum Shape { kMany, kFew, kF32 };
 
-
 struct CachedPlan {
   Shape shape;
   int tile_rows, unit_shift, min_share, extra, shares, merge_rows;
@@ -1154,7 +1155,9 @@ struct CachedPlan {
 // 700 x 1,500 x 24 40 / 31, single queries on 4,000 tokens x 40 18.6 / 23.8, on
 // 1,200 14.2 / 12.4.  (Within 5% of each other the estimate may miss: 6,000 x
 // 6,000 x 40 654 / 634.)  The bound of the lengths stands for the lengths, which
-// are device memory.
+// are device memory.  The costs are those of 128 channels, and of one workgroup
+// per compute unit in fp32; they stand for 64 channels, and for whole fp32 items,
+// of which two run, as well.
 //
 // A share has at least 256 tokens (with 512, 42 rows x 3,628 tokens x 6 heads
 // took 20 us, now 16).  An item's cost beside its tokens, the latencies of
