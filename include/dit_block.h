@@ -473,7 +473,8 @@ dit_status dit_cache_store(const dit_kv_cache *cache, int block, const void *k, 
  * request's cached tokens, with query rows cu_q[r]..cu_q[r+1] (host array) and
  * query head h on key/value head h / (n_heads / n_kv_heads).  q, o, strides and
  * softmax_scale as for dit_attention_varlen; head_dim (64 or 128 in both
- * dtypes) and n_kv_heads, a divisor of n_heads, are the cache's.  A request
+ * dtypes) and n_kv_heads, a divisor of n_heads, are the cache's; n_heads *
+ * head_dim is below 2^31 (larger: DIT_ERR_UNSUPPORTED).  A request
  * without tokens gets rows of zeros; table rows from n_req on are not read.  A
  * batch without query rows does nothing (q and o may be NULL).
  * Scores, probabilities' sums and products are fp32: a score of minus infinity

@@ -723,6 +723,9 @@ dit_status check_cached_items(const dit_kv_cache* c, const int32_t* cu, int n_re
 dit_status check_cached_heads(const dit_kv_cache* c, int n_heads) {
   if (n_heads < 1 || n_heads % c->n_kv_heads)
     return fail(DIT_ERR_INVALID_ARG, "%d query heads over %d key/value heads", n_heads, c->n_kv_heads);
+  // (the kernels form a head's place in its row in 32 bits)
+  if ((int64_t)n_heads * c->head_dim > 0x7FFFFFFF)
+    return fail(DIT_ERR_UNSUPPORTED, "query rows of %lld values (at most 2^31 - 1)", (long long)n_heads * c->head_dim);
   return DIT_OK;
 }
 
