@@ -1214,6 +1214,7 @@ size_t cached_attention_ws(const CachedAttnArgs& p) {
 }
 
 hipError_t launch_cached_attention(const CachedAttnArgs& p, void* ws, hipStream_t s) {
+  if (p.q_gain && (p.head_dim != 128 || p.dtype != DIT_BF16)) return hipErrorInvalidValue;
   const CachedPlan pl = plan(p, cu_count());
   CachedWork w{};
   w.shares = pl.shares; w.unit_shift = pl.unit_shift; w.min_share = pl.min_share; w.extra = pl.extra;
@@ -1258,9 +1259,10 @@ hipError_t launch_cached_attention(const CachedAttnArgs& p, void* ws, hipStream_
     const bf16* q = (const bf16*)p.q;
     bf16* o = (bf16*)p.o;
     if (pl.shape == kF32) cached_attn_f32<HD, SHARES><<<grid, 64 * kKeyWaves, 0, s>>>((const float*)p.q, (float*)p.o, w);
-    else if (pl.shape == kFew && p.q_gain) cached_attn_few<HD, true, SHARES><<<grid, 64 * kKeyWaves, 0, s>>>(q, o, w);
-    else if (pl.shape == kFew) cached_attn_few<HD, false, SHARES><<<grid, 64 * kKeyWaves, 0, s>>>(q, o, w);
-    else if (p.q_gain) cached_attn_many<HD, true, SHARES><<<grid, 256, 0, s>>>(q, o, w);
+    else if (p.q_gain) {   // (the block's bf16 heads have 128 channels)
+      if (pl.shape == kFew) cached_attn_few<128, true, SHARES><<<grid, 64 * kKeyWaves, 0, s>>>(q, o, w);
+      else cached_attn_many<128, true, SHARES><<<grid, 256, 0, s>>>(q, o, w);
+    } else if (pl.shape == kFew) cached_attn_few<HD, false, SHARES><<<grid, 64 * kKeyWaves, 0, s>>>(q, o, w);
     else cached_attn_many<HD, false, SHARES><<<grid, 256, 0, s>>>(q, o, w);
     if constexpr (SHARES) {
       const unsigned blocks = (unsigned)items * (pl.tile_rows / pl.merge_rows);
