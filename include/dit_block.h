@@ -280,6 +280,76 @@ dit_status dit_debug_attention_shape(int waves);
 dit_status dit_debug_attention_plan(const int32_t *cu_q, const int32_t *cu_k, int n_req, int n_heads,
                                     int compute_units, int *waves, int *split_pieces, int *split_items);
 
+/* ------------------------------------------- Linears on 8-bit integers */
+
+/* A row y of fp32 values is held as int8 codes c and one fp32 scale s:
+ *   m = max(max|y|, 127 * 2^-100),  s = m / 127,  c = 127 y / m to nearest, ties to even,
+ * so |c| <= 127 and y = c s within half a step s / 2.  127 y / m is computed to
+ * 2^-16 (a value nearer to the middle between two codes may take either); of
+ * bf16 rows as they are, exactly.  A row with a value that is not finite gets
+ * the scale NaN and codes 0.  A row's codes
+ * and scale do not depend on the rows beside it.  Codes are the operands of
+ * dit_linear_i8: activations with one scale per token, and weights [out, in]
+ * with one per output channel -- their rows -- from the same calls.
+ *
+ * codes: int8, rows of a multiple of 16 values, 16-byte aligned.  scales: fp32
+ * [n_rows], 4-byte aligned.  What is written must not overlap what is read, but
+ * where a call says so (checked, DIT_ERR_INVALID_ARG).  Calls without rows do
+ * nothing, and their tensors may be NULL. */
+
+/* The codes of x [n_rows, width] (dtype; strides in elements).  width <= 2^22. */
+dit_status dit_quantize_rows(const void *x, int64_t x_row_stride, int64_t n_rows, int width,
+                             int8_t *codes, int64_t codes_row_stride, float *scales,
+                             dit_dtype dtype, hipStream_t stream);
+
+/* dit_adaln_modulate with the result as codes [n_rows, hidden]: the codes of
+ * LN(x[i]) * (1 + scale[r]) + shift[r], which is not rounded to dtype before.
+ * hidden <= 8192 (bf16) or 4096 (fp32), else DIT_ERR_UNSUPPORTED. */
+dit_status dit_adaln_modulate_i8(const void *x, const float *shift, const float *scale,
+                                 int64_t mod_stride, const int32_t *cu_seqlens, int n_req,
+                                 int hidden, float eps, int8_t *codes, float *scales,
+                                 dit_dtype dtype, hipStream_t stream);
+
+/* Root-mean-square norm with the residual's addition:
+ *   sum = x + z, rounded to dtype (z and sum NULL: sum is x, nothing written)
+ *   y = sum / sqrt(mean(sum^2) + eps) * gain     (gain [hidden], dtype)
+ * written to out (dtype), as codes and scales, or both; those not wanted are
+ * NULL.  All rows are dense, [n_rows, hidden]; the mean of squares is fp32, so
+ * it has to stay in range.  sum and out may each be x or z (the same address),
+ * but not each other.  hidden as for dit_adaln_modulate_i8; a multiple of 8
+ * (bf16) or 4 (fp32) suffices without codes. */
+dit_status dit_add_rms_norm(const void *x, const void *z, const void *gain, int64_t n_rows,
+                            int hidden, float eps, void *sum, void *out, int8_t *codes,
+                            float *scales, dit_dtype dtype, hipStream_t stream);
+
+/* dit_linear on codes: out = epilogue(z), z[m][n] = (sum_k a[m][k] w[n][k]) *
+ * a_scales[m] * w_scales[n] + bias[n], with a [M, K] and w [N, K] of int8 (any
+ * value, -128 too; strides lda and ldw, at most 2^22) and bias, out, res of
+ * dtype; the epilogues as for dit_linear.  The sum is exact (32-bit integers),
+ * the rest fp32, one rounding to dtype at the end: a row of a packed batch has
+ * the same bits as alone.  K is a multiple of 16, at most 131,056; N a multiple
+ * of 8; else DIT_ERR_UNSUPPORTED.  out may be res (the same address and
+ * stride). */
+dit_status dit_linear_i8(const int8_t *a, int64_t lda, const float *a_scales, const int8_t *w,
+                         int64_t ldw, const float *w_scales, const void *bias, void *out,
+                         int64_t ldo, int64_t M, int N, int K, dit_epilogue epi, const void *res,
+                         int64_t ldr, const float *gate, int64_t gate_stride,
+                         const int32_t *cu_seqlens, int n_req, dit_dtype dtype,
+                         hipStream_t stream);
+
+/* dit_linear_i8 computes output tiles as dit_linear does, or, for few rows,
+ * blocks of 16 channels whose sums over K are shared by a workgroup's waves.
+ * For tests and tuning: dit_debug_linear_i8_tile forces a tile (256 x 256, 256 x
+ * 192, 128 x 256, 128 x 192, 128 x 128; 16 x 16 for the kernel for few rows,
+ * where the call has at most 4,096 of them) for every later call of this process,
+ * 0 x 0 restores the choice per shape; other values give DIT_ERR_INVALID_ARG.
+ * Results do not depend on it.  Process-wide; set it between calls.
+ * dit_debug_linear_i8_plan: the tile that a call takes on a GPU of
+ * `compute_units` compute units (16, 32 or 64 x 16 for few rows).  Host
+ * arithmetic only. */
+dit_status dit_debug_linear_i8_tile(int tile_m, int tile_n);
+dit_status dit_debug_linear_i8_plan(int64_t M, int N, int K, int compute_units, int *tile_m, int *tile_n);
+
 /* In place on q and (if not NULL) k, each [rows, n_heads*head_dim] with row
  * stride `row_stride`: per-head RMSNorm with gains g_q / g_k (skipped when the
  * gain is NULL), then, if vl != NULL and the sections are not all 0, the

@@ -151,6 +151,12 @@ def lib() -> ctypes.CDLL:
         "dit_adaln_modulate": (i32, [vp, vp, vp, i64, PI, i32, i32, f32, vp, i32, vp]),
         "dit_layer_norm_affine": (i32, [vp, vp, vp, i64, i32, f32, vp, i32, vp]),
         "dit_linear": (i32, [vp, i64, vp, i64, vp, vp, i64, i64, i32, i32, i32, vp, i64, vp, i64, PI, i32, i32, vp]),
+        "dit_quantize_rows": (i32, [vp, i64, i64, i32, vp, i64, vp, i32, vp]),
+        "dit_adaln_modulate_i8": (i32, [vp, vp, vp, i64, vp, i32, i32, f32, vp, vp, i32, vp]),
+        "dit_add_rms_norm": (i32, [vp, vp, vp, i64, i32, f32, vp, vp, vp, vp, i32, vp]),
+        "dit_linear_i8": (i32, [vp, i64, vp, vp, i64, vp, vp, vp, i64, i64, i32, i32, i32, vp, i64, vp, i64, vp, i32, i32, vp]),
+        "dit_debug_linear_i8_tile": (i32, [i32, i32]),
+        "dit_debug_linear_i8_plan": (i32, [i64, i32, i32, i32, ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_int)]),
         "dit_qk_norm_rope": (i32, [vp, vp, i64, i64, i32, i32, vp, vp, f32, PI, f32, PV, i32, vp]),
         "dit_gated_residual": (i32, [vp, vp, vp, vp, i64, PI, i32, i32, vp, i32, vp]),
         "dit_text_kv_elems": (sz, [PM, PV]),
@@ -196,7 +202,9 @@ def exported_symbols() -> Sequence[str]:
     return [n for n in ("dit_block_workspace_size", "dit_block_forward", "dit_block_pre_attention",
                         "dit_block_post_attention", "dit_timestep_modulation",
                         "dit_timestep_modulation_noalloc", "dit_attention_varlen",
-                        "dit_adaln_modulate", "dit_layer_norm_affine", "dit_linear", "dit_qk_norm_rope",
+                        "dit_adaln_modulate", "dit_layer_norm_affine", "dit_linear", "dit_quantize_rows",
+                        "dit_adaln_modulate_i8", "dit_add_rms_norm", "dit_linear_i8", "dit_debug_linear_i8_tile",
+                        "dit_debug_linear_i8_plan", "dit_qk_norm_rope",
                         "dit_gated_residual", "dit_text_kv_elems", "dit_text_kv", "dit_denoise_workspace_size",
                         "dit_denoise_step", "dit_patchify", "dit_unpatchify_euler", "dit_cache_run_bound",
                         "dit_cache_tables", "dit_cache_store", "dit_attention_cached_workspace_size",
@@ -402,6 +410,108 @@ def gated_residual(x, z, bias, gate, gate_stride, cu_seqlens, out, stream=None):
     _check(lib().dit_gated_residual(_ptr(x), _ptr(z), _ptr(bias), _ptr(gate), gate_stride, _pi(cu), len(cu) - 1,
                                     x.shape[-1], _ptr(out), dtype_code(x.dtype), _stream(stream)),
            "dit_gated_residual")
+
+
+# ------------------------------------------------ Linears on 8-bit integers
+
+
+def _i8_stream(stream, first, *tensors):
+    """The stream's handle: the call's tensors and the stream are on the current GPU."""
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError(f"a tensor of {first.dtype} {tuple(first.shape)} is on {first.device}")
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors on {first.device} and, of {t.dtype} {tuple(t.shape)}, on {t.device}")
+    s = torch.accelerator.current_stream() if stream is None else stream
+    if s.device_index != dev or (stream is not None and torch.cuda.current_device() != dev):
+        raise ValueError(f"the tensors are on {first.device}, the stream on cuda:{s.device_index}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+    if stream is not None:
+        return stream.cuda_stream
+    return 0 if s.stream_id == 0 else torch.cuda.current_stream().cuda_stream   # the default stream's handle is 0
+
+
+def _vectors(t, name, count, width, stride):
+    """A tensor that holds `count` fp32 vectors of `width` values, `stride` values apart, from its address on."""
+    need = ((count - 1) * stride + width) if count else 0
+    held = 1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())) if t.numel() else 0
+    if t.dtype != torch.float32 or t.stride(-1) != 1 or held < need:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}; needed: {count} fp32 vectors of {width}, "
+                         f"{stride} apart")
+    return t
+
+
+def quantize_rows(x, codes, scales, stream=None):
+    """x: [rows, width] of any row stride; codes: int8 of that shape; scales: fp32 [rows]."""
+    rows, width = x.shape
+    xs, cs = _rows_of(x, "x", width), _rows_of(codes, "codes", width)
+    if codes.dtype != torch.int8 or codes.shape != x.shape:
+        raise ValueError(f"codes: {codes.dtype} {tuple(codes.shape)}, x is {tuple(x.shape)}")
+    _want(scales, "scales", torch.float32, (rows,))
+    s = _i8_stream(stream, x, codes, scales)
+    _check(lib().dit_quantize_rows(x.data_ptr(), xs, rows, width, codes.data_ptr(), cs, scales.data_ptr(),
+                                   dtype_code(x.dtype), s), "dit_quantize_rows")
+
+
+def adaln_modulate_i8(x, shift, scale, mod_stride, cu_seqlens, eps, codes, scales, stream=None):
+    """adaln_modulate with the result as codes (int8, x's shape) and scales (fp32 [rows])."""
+    cu = _i32(cu_seqlens)
+    rows, width = x.shape
+    _want(x, "x", x.dtype)
+    _want(codes, "codes", torch.int8, x.shape)
+    _want(scales, "scales", torch.float32, (rows,))
+    if cu[-1] != rows:
+        raise ValueError(f"cu_seqlens ends at {cu[-1]}, x has {rows} rows")
+    for t, name in ((shift, "shift"), (scale, "scale")):
+        _vectors(t, name, len(cu) - 1, width, mod_stride)
+    s = _i8_stream(stream, x, shift, scale, codes, scales)
+    _check(lib().dit_adaln_modulate_i8(x.data_ptr(), shift.data_ptr(), scale.data_ptr(), int(mod_stride),
+                                       cu.__array_interface__["data"][0], len(cu) - 1, width, eps, codes.data_ptr(),
+                                       scales.data_ptr(), dtype_code(x.dtype), s), "dit_adaln_modulate_i8")
+
+
+def add_rms_norm(x, z, gain, eps, sum=None, out=None, codes=None, scales=None, stream=None):
+    """sum = x + z (z and sum None: x itself); its norm as out, as codes (int8) and scales (fp32 [rows]), or both."""
+    rows, width = x.shape
+    for t, name in ((x, "x"), (z, "z"), (sum, "sum"), (out, "out")):
+        if t is not None:
+            _want(t, name, x.dtype, x.shape)
+    _want(gain, "gain", x.dtype, (width,))
+    if codes is not None:
+        _want(codes, "codes", torch.int8, x.shape)
+    if scales is not None:
+        _want(scales, "scales", torch.float32, (rows,))
+    s = _i8_stream(stream, x, z, gain, sum, out, codes, scales)
+    _check(lib().dit_add_rms_norm(x.data_ptr(), _at(z), gain.data_ptr(), rows, width, eps, _at(sum), _at(out), _at(codes),
+                                  _at(scales), dtype_code(x.dtype), s), "dit_add_rms_norm")
+
+
+def linear_i8(a, a_scales, w, w_scales, bias, out, epi=EPI_NONE, res=None, gate=None, gate_stride=0, cu_seqlens=None,
+              stream=None):
+    """linear on codes: a int8 [M, K] with a_scales fp32 [M], w int8 [N, K] with w_scales fp32 [N]; bias, out and res of
+    one type."""
+    (M, K), N = a.shape, w.shape[0]
+    if a.dtype != torch.int8 or w.dtype != torch.int8 or w.shape[1] != K or out.shape != (M, N):
+        raise ValueError(f"a: {a.dtype} {tuple(a.shape)}, w: {w.dtype} {tuple(w.shape)}, out: {tuple(out.shape)}")
+    lda, ldw, ldo = _rows_of(a, "a", K), _rows_of(w, "w", K), _rows_of(out, "out", N)
+    _want(a_scales, "a_scales", torch.float32, (M,))
+    _want(w_scales, "w_scales", torch.float32, (N,))
+    if bias is not None:
+        _want(bias, "bias", out.dtype, (N,))
+    ldr = 0
+    if res is not None:
+        ldr = _rows_of(res, "res", N)
+        if res.dtype != out.dtype or res.shape != out.shape:
+            raise ValueError(f"res: {res.dtype} {tuple(res.shape)}, out: {out.dtype} {tuple(out.shape)}")
+    cu = None if cu_seqlens is None else _i32(cu_seqlens)
+    if gate is not None and cu is not None:
+        _vectors(gate, "gate", len(cu) - 1, N, gate_stride)
+    s = _i8_stream(stream, a, a_scales, w, w_scales, bias, out, res, gate)
+    _check(lib().dit_linear_i8(a.data_ptr(), lda, a_scales.data_ptr(), w.data_ptr(), ldw, w_scales.data_ptr(), _at(bias),
+                               out.data_ptr(), ldo, M, N, K, epi, _at(res), ldr, _at(gate), int(gate_stride),
+                               None if cu is None else cu.__array_interface__["data"][0], 0 if cu is None else len(cu) - 1,
+                               dtype_code(out.dtype), s), "dit_linear_i8")
 
 
 # ------------------------------------------------------- the denoising step

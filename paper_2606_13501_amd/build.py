@@ -16,7 +16,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libditblock.so")
 
-SOURCES = ["gemm.hip", "attention.hip", "rowwise.hip", "latent.hip", "cache.hip", "cached_attention.hip",
+SOURCES = ["gemm.hip", "gemm_i8.hip", "attention.hip", "rowwise.hip", "rows_i8.hip", "latent.hip", "cache.hip", "cached_attention.hip",
            "api.cpp", "sim.cpp", "migrate.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -97,6 +97,49 @@ ReqTable single_req(int64_t n_rows) {
   return t;
 }
 
+// ---- rows of 8-bit codes
+
+constexpr int kI8MaxStride = 1 << 22;   // a tile's byte offsets stay below 2^30
+constexpr int kI8MaxK = 131056;         // 128 * 128 * K stays below 2^31
+
+// Scales need the alignment of their type only: those of some rows begin anywhere.
+dit_status check_f32(const float* p, const char* name) {
+  if (!p) return fail(DIT_ERR_INVALID_ARG, "%s is NULL", name);
+  if ((uintptr_t)p & 3u) return fail(DIT_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
+  return DIT_OK;
+}
+
+// What is written (two ranges) does not meet each other or what is read.
+dit_status check_apart(const Span& a, const char* a_name, const Span& b, const char* b_name, const Span& in, const char* name) {
+  if (overlaps(a, b)) return fail(DIT_ERR_INVALID_ARG, "%s overlaps %s", a_name, b_name);
+  if (overlaps(a, in)) return fail(DIT_ERR_INVALID_ARG, "%s overlaps %s", a_name, name);
+  if (overlaps(b, in)) return fail(DIT_ERR_INVALID_ARG, "%s overlaps %s", b_name, name);
+  return DIT_OK;
+}
+
+dit_status check_rows_i8(int64_t n_rows, int width, dit_dtype dtype, bool codes) {
+  if (n_rows < 0 || n_rows > 0x7FFFFFFF) return fail(DIT_ERR_INVALID_ARG, "n_rows %lld", (long long)n_rows);
+  const int step = codes ? 16 : dtype == DIT_BF16 ? 8 : 4;
+  if (width < step || width % step) return fail(DIT_ERR_INVALID_ARG, "rows of %d must be a positive multiple of %d wide", width, step);
+  return DIT_OK;
+}
+
+dit_status check_norm_width(int hidden, dit_dtype dtype, float eps) {
+  if (hidden > (dtype == DIT_BF16 ? 8192 : 4096)) return fail(DIT_ERR_UNSUPPORTED, "hidden %d too large", hidden);
+  if (!(eps > 0.f) || isinf(eps)) return fail(DIT_ERR_INVALID_ARG, "eps must be > 0 and finite");
+  return DIT_OK;
+}
+
+dit_status check_linear_i8_size(int64_t M, int N, int K) {
+  if (M < 0 || M > 0x7FFFFFFF || N < 1 || K < 1) return fail(DIT_ERR_INVALID_ARG, "bad GEMM size M=%lld N=%d K=%d", (long long)M, N, K);
+  if (K % 16 || N % 8 || K > kI8MaxK)
+    return fail(DIT_ERR_UNSUPPORTED, "the 8-bit GEMM needs K %% 16 == 0, K <= %d and N %% 8 == 0 (K=%d N=%d)", kI8MaxK, K, N);
+  // tile coordinates in 32 bits
+  if (M > 0x7FFFFF00 || N > 0x7FFFFF00 || (M / 128 + 1) * (N / 128 + 1) > 0x7FFFFFF8ll)
+    return fail(DIT_ERR_UNSUPPORTED, "M=%lld x N=%d outputs are too many tiles", (long long)M, N);
+  return DIT_OK;
+}
+
 bool rope_on(const int s[3]) { return s[0] != 0 || s[1] != 0 || s[2] != 0; }
 
 dit_status check_sections(const int s[3], int head_dim) {
@@ -1149,6 +1192,150 @@ dit_status dit_linear(const void* a, int64_t lda, const void* w, int64_t ldw, co
   }
   return run_linear(a, lda, w, ldw, bias, out, ldo, M, N, K, epi, res, ldr, gate, gate_stride, req, dtype, stream,
                     "linear");
+}
+
+dit_status dit_quantize_rows(const void* x, int64_t x_row_stride, int64_t n_rows, int width, int8_t* codes,
+                             int64_t codes_row_stride, float* scales, dit_dtype dtype, hipStream_t stream) {
+  g_last_error.clear();
+  DIT_TRY(check_dtype(dtype));
+  DIT_TRY(check_rows_i8(n_rows, width, dtype, true));
+  if (width > kI8MaxStride) return fail(DIT_ERR_UNSUPPORTED, "width %d too large", width);
+  const int64_t vec = dtype == DIT_BF16 ? 8 : 4;
+  if (x_row_stride < width || x_row_stride % vec) return fail(DIT_ERR_INVALID_ARG, "x_row_stride %lld", (long long)x_row_stride);
+  if (codes_row_stride < width || codes_row_stride % 16) return fail(DIT_ERR_INVALID_ARG, "codes_row_stride %lld", (long long)codes_row_stride);
+  if (n_rows == 0) return DIT_OK;
+  DIT_TRY(check_ptr(x, "x")); DIT_TRY(check_ptr(codes, "codes")); DIT_TRY(check_f32(scales, "scales"));
+  const Span xs = span(x, n_rows, x_row_stride, width, elem_size(dtype));
+  DIT_TRY(check_apart(span(codes, n_rows, codes_row_stride, width, 1), "codes", span(scales, n_rows, 1, 1, 4), "scales", xs, "x"));
+  RowsI8Args p;
+  memset(&p, 0, sizeof(p));
+  p.op = RowOp::kRows; p.x = x; p.x_stride = x_row_stride; p.codes = codes; p.codes_stride = codes_row_stride;
+  p.scales = scales; p.n_rows = n_rows; p.width = width; p.dtype = dtype;
+  return hip_status(launch_rows_i8(p, stream), "quantize_rows");
+}
+
+dit_status dit_adaln_modulate_i8(const void* x, const float* shift, const float* scale, int64_t mod_stride,
+                                 const int32_t* cu_seqlens, int n_req, int hidden, float eps, int8_t* codes, float* scales,
+                                 dit_dtype dtype, hipStream_t stream) {
+  g_last_error.clear();
+  DIT_TRY(check_dtype(dtype));
+  DIT_TRY(check_cu(cu_seqlens, n_req, "cu_seqlens"));
+  const int64_t n_rows = cu_seqlens[n_req];
+  DIT_TRY(check_rows_i8(n_rows, hidden, dtype, true));
+  DIT_TRY(check_norm_width(hidden, dtype, eps));
+  if (mod_stride < 0 || mod_stride % 4) return fail(DIT_ERR_INVALID_ARG, "mod_stride %lld must be a multiple of 4 and >= 0", (long long)mod_stride);
+  if (n_rows == 0) return DIT_OK;
+  DIT_TRY(check_ptr(x, "x")); DIT_TRY(check_ptr(shift, "shift")); DIT_TRY(check_ptr(scale, "scale"));
+  DIT_TRY(check_ptr(codes, "codes")); DIT_TRY(check_f32(scales, "scales"));
+  const Span cs = span(codes, n_rows, hidden, hidden, 1), ss = span(scales, n_rows, 1, 1, 4);
+  DIT_TRY(check_apart(cs, "codes", ss, "scales", span(x, n_rows, hidden, hidden, elem_size(dtype)), "x"));
+  DIT_TRY(check_apart(cs, "codes", ss, "scales", span(shift, n_req, mod_stride, hidden, 4), "shift"));
+  DIT_TRY(check_apart(cs, "codes", ss, "scales", span(scale, n_req, mod_stride, hidden, 4), "scale"));
+  RowsI8Args p;
+  memset(&p, 0, sizeof(p));
+  p.op = RowOp::kModulate; p.x = x; p.codes = codes; p.scales = scales; p.n_rows = n_rows; p.width = hidden; p.eps = eps;
+  p.shift = shift; p.scale = scale; p.mod_stride = mod_stride; p.req = make_req(cu_seqlens, n_req); p.dtype = dtype;
+  return hip_status(launch_rows_i8(p, stream), "adaln_modulate_i8");
+}
+
+dit_status dit_add_rms_norm(const void* x, const void* z, const void* gain, int64_t n_rows, int hidden, float eps, void* sum,
+                            void* out, int8_t* codes, float* scales, dit_dtype dtype, hipStream_t stream) {
+  g_last_error.clear();
+  DIT_TRY(check_dtype(dtype));
+  DIT_TRY(check_rows_i8(n_rows, hidden, dtype, codes != nullptr || scales != nullptr));
+  DIT_TRY(check_norm_width(hidden, dtype, eps));
+  if (n_rows == 0) return DIT_OK;
+  DIT_TRY(check_ptr(x, "x")); DIT_TRY(check_ptr(gain, "gain")); DIT_TRY(check_ptr(z, "z", true));
+  DIT_TRY(check_ptr(sum, "sum", true)); DIT_TRY(check_ptr(out, "out", true)); DIT_TRY(check_ptr(codes, "codes", true));
+  if ((z == nullptr) != (sum == nullptr)) return fail(DIT_ERR_INVALID_ARG, "z and sum go together");
+  if ((codes == nullptr) != (scales == nullptr)) return fail(DIT_ERR_INVALID_ARG, "codes and scales go together");
+  if (!out && !codes) return fail(DIT_ERR_INVALID_ARG, "neither out nor codes is given");
+  if (codes) DIT_TRY(check_f32(scales, "scales"));
+  const int64_t es = elem_size(dtype);
+  auto rows = [&](const void* p) { return span(p, p ? n_rows : 0, hidden, hidden, es); };
+  const Span cs = span(codes, codes ? n_rows : 0, hidden, hidden, 1), ss = span(scales, scales ? n_rows : 0, 1, 1, 4);
+  const Span gs = span(gain, 1, hidden, hidden, es);
+  DIT_TRY(check_apart(cs, "codes", ss, "scales", rows(x), "x"));
+  DIT_TRY(check_apart(cs, "codes", ss, "scales", rows(z), "z"));
+  DIT_TRY(check_apart(cs, "codes", ss, "scales", rows(sum), "sum"));
+  DIT_TRY(check_apart(cs, "codes", ss, "scales", rows(out), "out"));
+  DIT_TRY(check_apart(cs, "codes", ss, "scales", gs, "gain"));
+  DIT_TRY(check_apart(rows(sum), "sum", rows(out), "out", gs, "gain"));
+  // rows are read whole before they are written: sum and out may each be x or z, but not lie across them
+  for (const void* in : {x, z}) {
+    if (sum && in && sum != in && overlaps(rows(sum), rows(in))) return fail(DIT_ERR_INVALID_ARG, "sum overlaps an input without being it");
+    if (out && in && out != in && overlaps(rows(out), rows(in))) return fail(DIT_ERR_INVALID_ARG, "out overlaps an input without being it");
+  }
+  RowsI8Args p;
+  memset(&p, 0, sizeof(p));
+  p.op = RowOp::kRms; p.x = x; p.z = z; p.gain = gain; p.sum = sum; p.out = out; p.codes = codes; p.scales = scales;
+  p.n_rows = n_rows; p.width = hidden; p.eps = eps; p.dtype = dtype;
+  return hip_status(launch_rows_i8(p, stream), "add_rms_norm");
+}
+
+dit_status dit_linear_i8(const int8_t* a, int64_t lda, const float* a_scales, const int8_t* w, int64_t ldw,
+                         const float* w_scales, const void* bias, void* out, int64_t ldo, int64_t M, int N, int K,
+                         dit_epilogue epi, const void* res, int64_t ldr, const float* gate, int64_t gate_stride,
+                         const int32_t* cu_seqlens, int n_req, dit_dtype dtype, hipStream_t stream) {
+  g_last_error.clear();
+  DIT_TRY(check_dtype(dtype));
+  DIT_TRY(check_linear_i8_size(M, N, K));
+  if (epi < DIT_EPI_NONE || epi > DIT_EPI_GATED_RESIDUAL) return fail(DIT_ERR_INVALID_ARG, "epilogue %d", (int)epi);
+  if (lda < K || ldw < K || lda % 16 || ldw % 16 || lda > kI8MaxStride || ldw > kI8MaxStride)
+    return fail(DIT_ERR_INVALID_ARG, "lda and ldw must cover the row, be multiples of 16 and at most %d", kI8MaxStride);
+  const int64_t vec = dtype == DIT_BF16 ? 8 : 4, es = elem_size(dtype);
+  if (ldo < N || ldo % vec) return fail(DIT_ERR_INVALID_ARG, "ldo must cover the row and be a multiple of %lld", (long long)vec);
+  const bool has_res = epi == DIT_EPI_RESIDUAL || epi == DIT_EPI_GATED_RESIDUAL;
+  if (has_res && (ldr < N || ldr % vec)) return fail(DIT_ERR_INVALID_ARG, "ldr %lld", (long long)ldr);
+  ReqTable req = single_req(M);
+  if (epi == DIT_EPI_GATED_RESIDUAL) {
+    if (gate_stride < 0 || gate_stride % 4) return fail(DIT_ERR_INVALID_ARG, "gate_stride %lld", (long long)gate_stride);
+    DIT_TRY(check_cu(cu_seqlens, n_req, "cu_seqlens"));
+    if (cu_seqlens[n_req] != M) return fail(DIT_ERR_INVALID_ARG, "cu_seqlens ends at %d, M is %lld", cu_seqlens[n_req], (long long)M);
+    req = make_req(cu_seqlens, n_req);
+  }
+  if (M == 0) return DIT_OK;
+  DIT_TRY(check_ptr(a, "a")); DIT_TRY(check_ptr(w, "w")); DIT_TRY(check_ptr(out, "out"));
+  DIT_TRY(check_f32(a_scales, "a_scales")); DIT_TRY(check_f32(w_scales, "w_scales"));
+  DIT_TRY(check_ptr(bias, "bias", true));
+  const Span os = span(out, M, ldo, N, es), none = {0, 0};
+  DIT_TRY(check_apart(os, "out", none, "", span(a, M, lda, K, 1), "a"));
+  DIT_TRY(check_apart(os, "out", none, "", span(w, N, ldw, K, 1), "w"));
+  DIT_TRY(check_apart(os, "out", none, "", span(a_scales, M, 1, 1, 4), "a_scales"));
+  DIT_TRY(check_apart(os, "out", none, "", span(w_scales, N, 1, 1, 4), "w_scales"));
+  DIT_TRY(check_apart(os, "out", none, "", span(bias, bias ? 1 : 0, N, N, es), "bias"));
+  if (has_res) {
+    DIT_TRY(check_ptr(res, "res"));
+    // out itself, columns of one buffer beside out's, or elsewhere
+    const int64_t step = ((const char*)res - (const char*)out) / es % ldo, off = step < 0 ? step + ldo : step;
+    const bool beside = ldr == ldo && off >= N && off <= ldo - N;
+    if (!(res == out && ldr == ldo) && !beside && overlaps(os, span(res, M, ldr, N, es)))
+      return fail(DIT_ERR_INVALID_ARG, "out overlaps res without being it");
+  }
+  if (epi == DIT_EPI_GATED_RESIDUAL) {
+    DIT_TRY(check_ptr(gate, "gate"));
+    DIT_TRY(check_apart(os, "out", none, "", span(gate, n_req, gate_stride, N, 4), "gate"));
+  }
+  LinearI8Args p;
+  p.a = a; p.lda = lda; p.a_scales = a_scales; p.w = w; p.ldw = ldw; p.w_scales = w_scales; p.bias = bias;
+  p.out = out; p.ldo = ldo; p.M = M; p.N = N; p.K = K; p.epi = epi; p.res = res; p.ldr = ldr;
+  p.gate = gate; p.gate_stride = gate_stride; p.req = req; p.dtype = dtype;
+  return hip_status(launch_linear_i8(p, stream), "linear_i8");
+}
+
+dit_status dit_debug_linear_i8_tile(int tile_m, int tile_n) {
+  g_last_error.clear();
+  if (!set_linear_i8_tile(tile_m, tile_n)) return fail(DIT_ERR_INVALID_ARG, "no output tile of %d x %d", tile_m, tile_n);
+  return DIT_OK;
+}
+
+dit_status dit_debug_linear_i8_plan(int64_t M, int N, int K, int compute_units, int* tile_m, int* tile_n) {
+  g_last_error.clear();
+  if (!tile_m || !tile_n) return fail(DIT_ERR_INVALID_ARG, "tile_m or tile_n is NULL");
+  if (M < 1 || compute_units < 1) return fail(DIT_ERR_INVALID_ARG, "M %lld, compute_units %d", (long long)M, compute_units);
+  DIT_TRY(check_linear_i8_size(M, N, K));
+  linear_i8_plan(M, N, K, compute_units, tile_m, tile_n);
+  return DIT_OK;
 }
 
 dit_status dit_qk_norm_rope(void* q, void* k, int64_t row_stride, int64_t n_rows, int n_heads, int head_dim,

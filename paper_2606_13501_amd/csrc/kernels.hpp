@@ -35,6 +35,28 @@ void set_gemm_tile_n(int bn);
 // The output tile of a bf16 GEMM on `cus` compute units.
 void gemm_plan(int64_t M, int N, int K, int cus, int* tile_m, int* tile_n);
 
+// Linears on 8-bit integers: rows of codes with a scale each, fp32.
+struct LinearI8Args {
+  const int8_t* a; int64_t lda;
+  const float* a_scales;         // [M]
+  const int8_t* w; int64_t ldw;
+  const float* w_scales;         // [N]
+  const void* bias;
+  void* out; int64_t ldo;
+  int64_t M; int N; int K;
+  dit_epilogue epi;
+  const void* res; int64_t ldr;
+  const float* gate; int64_t gate_stride;
+  ReqTable req;
+  dit_dtype dtype;               // of bias, res and out
+};
+hipError_t launch_linear_i8(const LinearI8Args& p, hipStream_t s);
+// Forces its output tile (16 x 16: the kernel for few rows; 0 x 0: chosen per
+// shape); false if there is none of that size.
+bool set_linear_i8_tile(int tile_m, int tile_n);
+// The output tile of a launch on `cus` compute units.
+void linear_i8_plan(int64_t M, int N, int K, int cus, int* tile_m, int* tile_n);
+
 struct AttnArgs {
   const void *q, *k, *v;
   void* o;
@@ -78,6 +100,25 @@ struct LnArgs {
   dit_dtype dtype;
 };
 hipError_t launch_layer_norm(const LnArgs& p, hipStream_t s);
+
+// Rows in 8 bits: a row y is written as int8 codes c and one fp32 scale s with
+// y ~ c s.  kRows: y = x; kModulate: y = LN(x) (1 + scale) + shift per request;
+// kRms: sum = x + z (z NULL: sum = x, not written), y = sum / rms(sum) * gain,
+// written as out and / or as codes.
+enum class RowOp { kRows, kModulate, kRms };
+struct RowsI8Args {
+  RowOp op;
+  const void* x; int64_t x_stride;      // elements
+  int8_t* codes; int64_t codes_stride;  // NULL: no codes (kRms)
+  float* scales;
+  int64_t n_rows; int width;
+  float eps;
+  const float* shift; const float* scale; int64_t mod_stride;   // kModulate
+  const void* z; const void* gain; void* sum; void* out;        // kRms, dense rows
+  ReqTable req;
+  dit_dtype dtype;
+};
+hipError_t launch_rows_i8(const RowsI8Args& p, hipStream_t s);
 
 struct NormRopeArgs {
   void* q; void* k;

@@ -1,0 +1,399 @@
+// Rows in 8 bits, the operand of the Linears on 8-bit integers: a row y is
+// written as int8 codes c and one fp32 scale s,
+//   m = max(max|y|, 127 x 2^-100),  s = m / 127,  c = 127 y / m to nearest, ties to even,
+// so that |c| <= 127 and y = c s within s / 2.  The row y is an activation or a
+// weight as it is, the modulated LayerNorm of one, or the root-mean-square norm
+// of a sum.  It is formed and kept in fp32: rounded to bf16 first, a value next
+// to the largest would be off by 2^-9 of it before the codes round it by 2^-8.
+// A row with a value that is not finite gets the scale NaN and codes of 0: what
+// is computed from it is NaN.
+//
+// The kernels are bound by memory: a wave holds a row in registers from its one
+// read to its one write (as the norms of 16-bit rows do).
+#include "common.hpp"
+#include "kernels.hpp"
+#include "rows.hpp"
+
+namespace dit {
+
+namespace {
+
+constexpr float kLeastTop = 127.0f * 0x1p-100f;
+constexpr int64_t kMaxGroups = 1 << 22;   // workgroups of a launch: 2^30 work-items; more rows take turns
+
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, kWave));
+  return v;
+}
+
+// How a row is scaled, from the bits of its largest magnitude (those of
+// infinity and of every NaN are above the finite ones).
+struct RowScale {
+  float s;        // what is written
+  float hi, lo;   // 127 / m in two parts
+  bool fine;      // all values are finite
+  __device__ explicit RowScale(uint32_t top) {
+    const float m = fmaxf(__uint_as_float(top), kLeastTop);
+    fine = top < 0x7F800000u;
+    s = fine ? m / 127.0f : __uint_as_float(0x7FC00000u);
+    hi = 127.0f / m;
+    lo = fmaf(-hi, m, 127.0f) / m;
+  }
+};
+
+// VN codes as bytes: z + 1.5 x 2^23 leaves z, rounded to nearest even, in the
+// low bits of the sum, two's complement.  The codes of rows as they are (TIES)
+// take z = fl(y hi + y lo), which is 127 y / m rounded once to fp32 but for a
+// part in 2^22 of the step between fp32 numbers: bf16 rows are often exactly in
+// the middle between two codes (127 y / m = k + 1/2 for two numbers of 8 bits),
+// and with 1 / s rounded such values went to either side (1 in 10,000 codes was
+// off by one).  A norm's values are not such numbers: z = y hi inside the sum.
+template <int VN> struct CodeVec;
+template <> struct CodeVec<8> { typedef u32x2 type; };
+template <> struct CodeVec<4> { typedef uint32_t type; };
+
+template <bool TIES>
+__device__ __forceinline__ uint32_t codes4(const float* y, const RowScale& q) {
+  uint32_t u[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    u[e] = __float_as_uint(TIES ? fmaf(y[e], q.hi, y[e] * q.lo) + 12582912.0f : fmaf(y[e], q.hi, 12582912.0f));
+  const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0400u);   // bytes: u0, u1, 0, 0
+  const uint32_t hi = __builtin_amdgcn_perm(u[3], u[2], 0x04000C0Cu);   // 0, 0, u2, u3
+  return q.fine ? lo | hi : 0u;
+}
+
+template <int VN, bool TIES>
+__device__ __forceinline__ void store_codes(int8_t* at, const float (&y)[VN], const RowScale& q) {
+  typename CodeVec<VN>::type o;
+  if constexpr (VN == 8) {
+    o[0] = codes4<TIES>(y, q);
+    o[1] = codes4<TIES>(y + 4, q);
+  } else {
+    o = codes4<TIES>(y, q);
+  }
+  __builtin_nontemporal_store(o, reinterpret_cast<typename CodeVec<VN>::type*>(at));
+}
+
+// The largest magnitude of a row held by WPR waves (their workgroup): each has
+// `top` of its part.
+template <int WPR>
+__device__ __forceinline__ uint32_t row_top(uint32_t top) {
+  top = wave_max(top);
+  if constexpr (WPR > 1) {
+    __shared__ uint32_t tops[WPR];
+    __syncthreads();   // the last row's are read
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) top = max(top, tops[w]);
+  }
+  return top;
+}
+
+// y = x.  WPR waves per row (1: four rows per workgroup; 4: one).
+template <typename T, int NVL, int WPR>
+__global__ __launch_bounds__(256) void rows_i8_kernel(const T* __restrict__ x, int64_t x_stride, int8_t* __restrict__ codes,
+                                                      int64_t codes_stride, float* __restrict__ scales, int64_t n_rows,
+                                                      int width) {
+  typedef typename Vec16<T>::type V;
+  constexpr int VN = Vec16<T>::n, RPW = 4 / WPR;
+  const int t = threadIdx.x & (64 * WPR - 1);   // thread of the row
+  const int nv = width / VN;
+  for (int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / (64 * WPR); row < n_rows; row += (int64_t)gridDim.x * RPW) {
+    const T* xr = x + row * x_stride;
+    V v[NVL];
+#pragma unroll
+    for (int i = 0; i < NVL; ++i) {
+      const int c = t + 64 * WPR * i;
+      v[i] = c < nv ? __builtin_nontemporal_load(reinterpret_cast<const V*>(xr + c * VN)) : V{};
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < NVL; ++i)
+#pragma unroll
+      for (int e = 0; e < VN; ++e) top = max(top, magnitude(to_f<T>(v[i][e])));
+    top = row_top<WPR>(top);
+    const RowScale q(top);
+    if (t == 0) scales[row] = q.s;
+    int8_t* cr = codes + row * codes_stride;
+#pragma unroll
+    for (int i = 0; i < NVL; ++i) {
+      const int c = t + 64 * WPR * i;
+      if (c < nv) {
+        float y[VN];
+#pragma unroll
+        for (int e = 0; e < VN; ++e) y[e] = to_f<T>(v[i][e]);
+        store_codes<VN, true>(cr + c * VN, y, q);
+      }
+    }
+  }
+}
+
+// y = x for rows that registers do not hold: read twice, the second time from the caches.
+template <typename T>
+__global__ __launch_bounds__(256) void rows_i8_wide_kernel(const T* __restrict__ x, int64_t x_stride,
+                                                           int8_t* __restrict__ codes, int64_t codes_stride,
+                                                           float* __restrict__ scales, int64_t n_rows, int width) {
+  typedef typename Vec16<T>::type V;
+  constexpr int VN = Vec16<T>::n, U = 4;
+  const int nv = width / VN;
+  for (int64_t row = blockIdx.x; row < n_rows; row += gridDim.x) {
+    const T* xr = x + row * x_stride;
+    uint32_t top = 0;
+    for (int c0 = threadIdx.x; c0 < nv; c0 += 256 * U) {
+      V v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + 256 * u;
+        v[u] = c < nv ? *reinterpret_cast<const V*>(xr + (int64_t)c * VN) : V{};
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < VN; ++e) top = max(top, magnitude(to_f<T>(v[u][e])));
+    }
+    top = row_top<4>(top);
+    const RowScale q(top);
+    if (threadIdx.x == 0) scales[row] = q.s;
+    int8_t* cr = codes + row * codes_stride;
+    for (int c = threadIdx.x; c < nv; c += 256) {
+      const V v = *reinterpret_cast<const V*>(xr + (int64_t)c * VN);
+      float y[VN];
+#pragma unroll
+      for (int e = 0; e < VN; ++e) y[e] = to_f<T>(v[e]);
+      store_codes<VN, true>(cr + (int64_t)c * VN, y, q);
+    }
+  }
+}
+
+// A wave's row y [NVL][VN] (zeros behind the row) as codes and scale.
+template <int NVL, int VN>
+__device__ __forceinline__ void emit_codes(const float (&y)[NVL][VN], int lane, int nv, int8_t* cr, float* scale) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < NVL; ++i)
+#pragma unroll
+    for (int e = 0; e < VN; ++e) top = max(top, magnitude(y[i][e]));
+  top = wave_max(top);
+  const RowScale q(top);
+  if (lane == 0) *scale = q.s;
+#pragma unroll
+  for (int i = 0; i < NVL; ++i)
+    if (lane + 64 * i < nv) store_codes<VN, false>(cr + (lane + 64 * i) * VN, y[i], q);
+}
+
+// y = LN(x) (1 + scale) + shift, a row per wave, four rows per workgroup: the
+// statistics and the staging of the request's vectors are those of the kernel
+// that writes y in the rows' own type (layer_norm_mod_kernel), and so is y.
+template <typename T, int NVL>
+__global__ __launch_bounds__(256) void modulate_i8_kernel(const T* __restrict__ x, int8_t* __restrict__ codes,
+                                                          float* __restrict__ scales, int64_t n_rows, int hidden, float eps,
+                                                          const float* __restrict__ shift, const float* __restrict__ scale,
+                                                          int64_t mod_stride, ReqTable req) {
+  typedef typename Vec16<T>::type V;
+  constexpr int VN = Vec16<T>::n, G = VN / 4;
+  extern __shared__ f32x4 smod[];   // hidden / 4 vectors of 1 + scale, then of shift: vector G c + g at g nv + c
+  const int lane = threadIdx.x & 63;
+  const int nv = hidden / VN, h4 = hidden / 4;
+  for (int64_t r0 = (int64_t)blockIdx.x * 4; r0 < n_rows; r0 += (int64_t)gridDim.x * 4) {
+    const int64_t row = r0 + (threadIdx.x >> 6);
+    const int ra = find_req(req.cu, req.n_req, (int)r0);
+    const bool staged = ra == find_req(req.cu, req.n_req, (int)(min(r0 + 4, n_rows) - 1));   // one request's rows
+    __syncthreads();   // the last rows' vectors are read
+    if (staged) {
+      const f32x4* sc = reinterpret_cast<const f32x4*>(scale + (int64_t)ra * mod_stride);
+      const f32x4* sh = reinterpret_cast<const f32x4*>(shift + (int64_t)ra * mod_stride);
+      for (int at = threadIdx.x; at < h4; at += 256) {
+        const int i = G * (at % nv) + at / nv;
+        f32x4 m = sc[i];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) m[u] = 1.0f + m[u];
+        smod[at] = m;
+        smod[h4 + at] = sh[i];
+      }
+      __syncthreads();
+    }
+    if (row >= n_rows) continue;
+    float y[NVL][VN];
+    {
+      V v[NVL];
+      const T* xr = x + row * hidden;
+#pragma unroll
+      for (int i = 0; i < NVL; ++i) {
+        const int c = lane + 64 * i;
+        v[i] = c < nv ? __builtin_nontemporal_load(reinterpret_cast<const V*>(xr + c * VN)) : V{};
+      }
+      float mean, rstd;
+      row_stats<T, NVL>(v, lane, nv, hidden, eps, mean, rstd);
+      const int r = staged ? ra : find_req(req.cu, req.n_req, (int)row);
+      const f32x4* sc = reinterpret_cast<const f32x4*>(scale + (int64_t)r * mod_stride);
+      const f32x4* sh = reinterpret_cast<const f32x4*>(shift + (int64_t)r * mod_stride);
+      auto form = [&](auto&& mul_add) {
+#pragma unroll
+        for (int i = 0; i < NVL; ++i) {
+          const int c = lane + 64 * i;
+#pragma unroll
+          for (int e = 0; e < VN; e += 4) {
+            f32x4 m4{}, a4{};
+            if (c < nv) mul_add((c * VN + e) / 4, m4, a4);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              y[i][e + u] = c < nv ? fmaf((to_f<T>(v[i][e + u]) - mean) * rstd, m4[u], a4[u]) : 0.f;
+          }
+        }
+      };
+      if (staged) {
+        form([&](int j, f32x4& m4, f32x4& a4) {
+          const int at = (j % G) * nv + j / G;
+          m4 = smod[at];
+          a4 = smod[h4 + at];
+        });
+      } else {
+        form([&](int j, f32x4& m4, f32x4& a4) {
+          m4 = sc[j];
+          a4 = sh[j];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) m4[u] = 1.0f + m4[u];
+        });
+      }
+    }
+    emit_codes<NVL, VN>(y, lane, nv, codes + row * hidden, scales + row);
+  }
+}
+
+// sum = x + z rounded to T (z NULL: x itself), y = sum / sqrt(mean(sum^2) + eps)
+// * gain, a row per wave.  The norm is that of the rounded sum, which is what
+// the residual stream goes on with.  sum may be x or z, and out x or z: a row
+// is read by the wave that writes it, before.
+template <typename T, int NVL>
+__global__ __launch_bounds__(256) void add_rms_kernel(const T* x, const T* z, const T* __restrict__ gain, T* sum, T* out,
+                                                      int8_t* __restrict__ codes, float* __restrict__ scales, int64_t n_rows,
+                                                      int hidden, float eps) {
+  typedef typename Vec16<T>::type V;
+  constexpr int VN = Vec16<T>::n;
+  const int lane = threadIdx.x & 63;
+  const int nv = hidden / VN;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < n_rows; row += (int64_t)gridDim.x * 4) {
+    const int64_t at = row * hidden;
+    V v[NVL];
+#pragma unroll
+    for (int i = 0; i < NVL; ++i) {
+      const int c = lane + 64 * i;
+      v[i] = c < nv ? __builtin_nontemporal_load(reinterpret_cast<const V*>(x + at + c * VN)) : V{};
+    }
+    if (z) {
+      V w[NVL];
+#pragma unroll
+      for (int i = 0; i < NVL; ++i) {
+        const int c = lane + 64 * i;
+        w[i] = c < nv ? __builtin_nontemporal_load(reinterpret_cast<const V*>(z + at + c * VN)) : V{};
+      }
+#pragma unroll
+      for (int i = 0; i < NVL; ++i) {
+        const int c = lane + 64 * i;
+#pragma unroll
+        for (int e = 0; e < VN; ++e) v[i][e] = from_f<T>(to_f<T>(v[i][e]) + to_f<T>(w[i][e]));
+        if (c < nv) __builtin_nontemporal_store(v[i], reinterpret_cast<V*>(sum + at + c * VN));
+      }
+    }
+    float sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < NVL; ++i)
+#pragma unroll
+      for (int e = 0; e < VN; ++e) {
+        const float f = to_f<T>(v[i][e]);
+        sq = fmaf(f, f, sq);
+      }
+    const float rs = rsqrtf(wave_sum(sq) / hidden + eps);
+    float y[NVL][VN];
+#pragma unroll
+    for (int i = 0; i < NVL; ++i) {
+      const int c = lane + 64 * i;
+      V g{};
+      if (c < nv) g = *reinterpret_cast<const V*>(gain + c * VN);
+#pragma unroll
+      for (int e = 0; e < VN; ++e) y[i][e] = c < nv ? to_f<T>(v[i][e]) * rs * to_f<T>(g[e]) : 0.f;
+    }
+    if (out) {
+#pragma unroll
+      for (int i = 0; i < NVL; ++i) {
+        const int c = lane + 64 * i;
+        V o;
+#pragma unroll
+        for (int e = 0; e < VN; ++e) o[e] = from_f<T>(y[i][e]);
+        if (c < nv) __builtin_nontemporal_store(o, reinterpret_cast<V*>(out + at + c * VN));
+      }
+    }
+    if (codes) emit_codes<NVL, VN>(y, lane, nv, codes + at, scales + row);
+  }
+}
+
+unsigned groups(int64_t n) { return (unsigned)(n < kMaxGroups ? n : kMaxGroups); }
+
+template <typename T, int NVL>
+hipError_t norm_nvl(const RowsI8Args& p, hipStream_t s) {
+  const unsigned grid = groups((p.n_rows + 3) / 4);
+  if (p.op == RowOp::kModulate)
+    modulate_i8_kernel<T, NVL><<<grid, 256, (size_t)p.width * 8, s>>>((const T*)p.x, p.codes, p.scales, p.n_rows, p.width,
+                                                                       p.eps, p.shift, p.scale, p.mod_stride, p.req);
+  else if (p.op == RowOp::kRms)
+    add_rms_kernel<T, NVL><<<grid, 256, 0, s>>>((const T*)p.x, (const T*)p.z, (const T*)p.gain, (T*)p.sum, (T*)p.out,
+                                                p.codes, p.scales, p.n_rows, p.width, p.eps);
+  else
+    rows_i8_kernel<T, NVL, 1><<<grid, 256, 0, s>>>((const T*)p.x, p.x_stride, p.codes, p.codes_stride, p.scales, p.n_rows,
+                                                   p.width);
+  return hipGetLastError();
+}
+
+template <typename T, int NVL>
+hipError_t rows_wg(const RowsI8Args& p, hipStream_t s) {
+  rows_i8_kernel<T, NVL, 4><<<groups(p.n_rows), 256, 0, s>>>((const T*)p.x, p.x_stride, p.codes, p.codes_stride, p.scales,
+                                                             p.n_rows, p.width);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t rows_typed(const RowsI8Args& p, hipStream_t s) {
+  const int nv = p.width / Vec16<T>::n;
+  switch ((nv + 63) / 64) {   // 16-byte vectors of a lane
+    case 1: return norm_nvl<T, 1>(p, s);
+    case 2: return norm_nvl<T, 2>(p, s);
+    case 3: return norm_nvl<T, 3>(p, s);
+    case 4: return norm_nvl<T, 4>(p, s);
+    case 5: return norm_nvl<T, 5>(p, s);
+    case 6: return norm_nvl<T, 6>(p, s);
+    case 7: return norm_nvl<T, 7>(p, s);
+    case 8: return norm_nvl<T, 8>(p, s);
+    case 9: case 10: return norm_nvl<T, 10>(p, s);
+    case 11: case 12: return norm_nvl<T, 12>(p, s);
+    case 13: case 14: return norm_nvl<T, 14>(p, s);
+    case 15: case 16: return norm_nvl<T, 16>(p, s);
+    default: break;
+  }
+  if (p.op != RowOp::kRows) return hipErrorInvalidValue;
+  switch ((nv + 255) / 256) {
+    case 5: return rows_wg<T, 5>(p, s);
+    case 6: return rows_wg<T, 6>(p, s);
+    case 7: return rows_wg<T, 7>(p, s);
+    case 8: return rows_wg<T, 8>(p, s);
+    case 9: case 10: case 11: case 12: return rows_wg<T, 12>(p, s);
+    case 13: case 14: case 15: case 16: return rows_wg<T, 16>(p, s);
+    default: break;
+  }
+  rows_i8_wide_kernel<T><<<groups(p.n_rows), 256, 0, s>>>((const T*)p.x, p.x_stride, p.codes, p.codes_stride, p.scales,
+                                                          p.n_rows, p.width);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rows_i8(const RowsI8Args& p, hipStream_t s) {
+  if (p.n_rows == 0) return hipSuccess;
+  return p.dtype == DIT_BF16 ? rows_typed<bf16>(p, s) : rows_typed<float>(p, s);
+}
+
+}  // namespace dit

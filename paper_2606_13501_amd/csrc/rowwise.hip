@@ -13,14 +13,11 @@
 
 #include "common.hpp"
 #include "kernels.hpp"
+#include "rows.hpp"
 
 namespace dit {
 
 namespace {
-
-template <typename T> struct Vec16;
-template <> struct Vec16<bf16> { typedef bf16x8 type; static constexpr int n = 8; };
-template <> struct Vec16<float> { typedef f32x4 type; static constexpr int n = 4; };
 
 // ------------------------------------------------------------ LayerNorm
 // out = (x - mean) / sqrt(var + eps) * mul + add, one wave per row.
@@ -28,33 +25,6 @@ template <> struct Vec16<float> { typedef f32x4 type; static constexpr int n = 4
 //   affine:   mul = gamma, add = beta (dtype vectors)
 // NVL = 16-byte vectors per lane, a compile-time count so the row is held in
 // exactly as many registers as it needs (occupancy hides the HBM latency).
-
-// Mean and 1 / sqrt(var + eps) of the wave's row v (NVL vectors per lane).
-// The squares are accumulated with explicit fused multiply-adds, so every
-// kernel that calls this rounds the statistics the same way.
-template <typename T, int NVL, typename V>
-__device__ __forceinline__ void row_stats(const V (&v)[NVL], int lane, int nv, int hidden, float eps, float& mean,
-                                          float& rstd) {
-  constexpr int VN = Vec16<T>::n;
-  float sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < NVL; ++i)
-#pragma unroll
-    for (int e = 0; e < VN; ++e) sum += to_f<T>(v[i][e]);
-  mean = wave_sum(sum) / hidden;
-  float sq = 0.f;
-#pragma unroll
-  for (int i = 0; i < NVL; ++i) {
-    if (lane + 64 * i < nv) {
-#pragma unroll
-      for (int e = 0; e < VN; ++e) {
-        const float d = to_f<T>(v[i][e]) - mean;
-        sq = fmaf(d, d, sq);
-      }
-    }
-  }
-  rstd = rsqrtf(wave_sum(sq) / hidden + eps);
-}
 
 template <typename T, int NVL>
 __global__ __launch_bounds__(256) void layer_norm_affine_kernel(
