@@ -100,6 +100,7 @@ ReqTable single_req(int64_t n_rows) {
 // ---- rows of 8-bit codes
 
 constexpr int kI8MaxStride = 1 << 22;   // a tile's byte offsets stay below 2^30
+constexpr int kI8MaxOut = 1 << 24;      // 16 output rows end below 2^31
 constexpr int kI8MaxK = 131056;         // 128 * 128 * K stays below 2^31
 
 // Scales need the alignment of their type only: those of some rows begin anywhere.
@@ -132,10 +133,11 @@ dit_status check_norm_width(int hidden, dit_dtype dtype, float eps) {
 
 dit_status check_linear_i8_size(int64_t M, int N, int K) {
   if (M < 0 || M > 0x7FFFFFFF || N < 1 || K < 1) return fail(DIT_ERR_INVALID_ARG, "bad GEMM size M=%lld N=%d K=%d", (long long)M, N, K);
-  if (K % 16 || N % 8 || K > kI8MaxK)
-    return fail(DIT_ERR_UNSUPPORTED, "the 8-bit GEMM needs K %% 16 == 0, K <= %d and N %% 8 == 0 (K=%d N=%d)", kI8MaxK, K, N);
+  if (K % 16 || N % 8 || K > kI8MaxK || N > kI8MaxOut)
+    return fail(DIT_ERR_UNSUPPORTED, "the 8-bit GEMM needs K %% 16 == 0, K <= %d, N %% 8 == 0 and N <= %d (K=%d N=%d)", kI8MaxK,
+                kI8MaxOut, K, N);
   // tile coordinates in 32 bits
-  if (M > 0x7FFFFF00 || N > 0x7FFFFF00 || (M / 128 + 1) * (N / 128 + 1) > 0x7FFFFFF8ll)
+  if (M > 0x7FFFFF00 || (M / 128 + 1) * (N / 128 + 1) > 0x7FFFFFF8ll)
     return fail(DIT_ERR_UNSUPPORTED, "M=%lld x N=%d outputs are too many tiles", (long long)M, N);
   return DIT_OK;
 }
@@ -1284,9 +1286,10 @@ dit_status dit_linear_i8(const int8_t* a, int64_t lda, const float* a_scales, co
   if (lda < K || ldw < K || lda % 16 || ldw % 16 || lda > kI8MaxStride || ldw > kI8MaxStride)
     return fail(DIT_ERR_INVALID_ARG, "lda and ldw must cover the row, be multiples of 16 and at most %d", kI8MaxStride);
   const int64_t vec = dtype == DIT_BF16 ? 8 : 4, es = elem_size(dtype);
-  if (ldo < N || ldo % vec) return fail(DIT_ERR_INVALID_ARG, "ldo must cover the row and be a multiple of %lld", (long long)vec);
+  if (ldo < N || ldo % vec || ldo > kI8MaxOut)
+    return fail(DIT_ERR_INVALID_ARG, "ldo must cover the row, be a multiple of %lld and at most %d", (long long)vec, kI8MaxOut);
   const bool has_res = epi == DIT_EPI_RESIDUAL || epi == DIT_EPI_GATED_RESIDUAL;
-  if (has_res && (ldr < N || ldr % vec)) return fail(DIT_ERR_INVALID_ARG, "ldr %lld", (long long)ldr);
+  if (has_res && (ldr < N || ldr % vec || ldr > kI8MaxOut)) return fail(DIT_ERR_INVALID_ARG, "ldr %lld", (long long)ldr);
   ReqTable req = single_req(M);
   if (epi == DIT_EPI_GATED_RESIDUAL) {
     if (gate_stride < 0 || gate_stride % 4) return fail(DIT_ERR_INVALID_ARG, "gate_stride %lld", (long long)gate_stride);

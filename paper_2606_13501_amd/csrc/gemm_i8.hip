@@ -24,13 +24,41 @@ template <typename T> struct Vec8;   // eight values of an output type
 template <> struct Vec8<bf16> { typedef bf16x8 type; };
 template <> struct Vec8<float> { typedef float type __attribute__((ext_vector_type(8), aligned(16))); };
 
-// c += w . a^T for one 16 x 16 block and 64 of K, in place in the accumulation
-// registers.  Inline assembly for the reason given at the bf16 kernel's; the
-// distances to the instructions that write and read the accumulators are kept
+// c += w . a^T (or c = w . a^T) for one 16 x 16 block and 64 of K, in place in
+// the accumulation registers.  Inline assembly for the reason given at the bf16
+// kernel's; the distance to the instructions that read the accumulators is kept
 // by hand.
 __device__ __forceinline__ void mfma16(i32x4& c, const i32x4& w, const i32x4& a) {
   asm("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(a));
 }
+__device__ __forceinline__ void mfma16_first(i32x4& c, const i32x4& w, const i32x4& a) {
+  asm("v_mfma_i32_16x16x64_i8 %0, %1, %2, 0" : "=a"(c) : "v"(w), "v"(a));
+}
+
+// A sum out of the accumulation registers, where it stands: left to the
+// compiler, the copies of all 256 would be made at once after the K loop, for
+// which the registers do not suffice.
+__device__ __forceinline__ int32_t sum_of(const i32x4& c, int e) {
+  int32_t v;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(c[e]));
+  return v;
+}
+
+// A load from global memory into LDS in two parts, an MFMA between them: the
+// address in LDS (m0), then the load itself (16 or 4 bytes a lane).  The vector
+// offset passes through the first part so that it is computed there too.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+template <int AT> __device__ __forceinline__ void load_lds_to(uint32_t lds, int& voff) {
+  asm volatile("s_add_u32 m0, %1, %2" : "+v"(voff) : "s"(lds), "n"(AT) : "m0", "scc");
+}
+__device__ __forceinline__ void load_lds_16(const u32x4& desc, int voff, int soff) {
+  asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" :: "v"(voff), "s"(desc), "s"(soff) : "m0");
+}
+__device__ __forceinline__ void load_lds_4(const u32x4& desc, int voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds), "v"(voff), "s"(desc) : "m0");
+}
+#pragma clang diagnostic pop
 
 // What an epilogue needs of the call.
 template <typename T>
@@ -53,6 +81,11 @@ struct Epi {
 // bytes per lane that v_mfma_f32_16x16x32_bf16 takes, in the same time, for
 // twice the products.
 //
+// channel_swizzle: the 16 lanes that read the rows 8 a + 4 h + c of W (a, c = 0
+// .. 3) at one logical chunk touch 16 distinct bank groups: rows of one parity
+// get 8 different chunks.
+__device__ __forceinline__ int channel_swizzle(int r) { return (((r >> 3) & 3) << 1) | ((r >> 1) & 1); }
+
 // K need not be whole steps: in the last one, the lanes whose 16 bytes lie
 // behind K load from an offset that no descriptor reaches, and get zeros.
 constexpr uint32_t kNowhere = 0x80000000u;
@@ -77,97 +110,141 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
   const int tail_chunks = (K - (KT - 1) * BK) / 16;   // 16-byte chunks of a row in the last step
 
   // ---- global -> LDS, as in the bf16 kernel: pieces of 8 rows x 128 bytes,
-  // lane i of piece q holds row 8 q + i / 8, logical chunk (i % 8) ^
-  // row_swizzle(row).  A tile's descriptor ends with the operand's last row, or
+  // lane i of piece q holds row 8 q + i / 8, logical chunk (i % 8) ^ the row's
+  // swizzle: row_swizzle for A, whose swizzle is that of the parity of q, and
+  // channel_swizzle for W, of q mod 4.  A tile's descriptor ends with the operand's last row, or
   // 2 GiB on: a tile's own rows end before (row strides are at most 2^22).
   static_assert(LA % 2 == 0 && LW % 2 == 0, "the parity of a piece is that of its index in the wave");
-  int a_vo[2], w_vo[2], behind[2];   // behind: kNowhere if the lane's chunk of the last step is behind K
-#pragma unroll
-  for (int par = 0; par < 2; ++par) {
-    const int c = (lane & 7) ^ (4 * par + (lane >> 4));
-    a_vo[par] = (LA * wave * 8 + (lane >> 3)) * (int)lda + c * 16;
-    w_vo[par] = (LW * wave * 8 + (lane >> 3)) * (int)ldw + c * 16;
-    behind[par] = c < tail_chunks ? 0 : (int)kNowhere;
-  }
   const int a_pc = 8 * (int)lda, w_pc = 8 * (int)ldw;   // bytes of 8 rows
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  // the load cursor: step l_step of the sequence's tile l_it, and the lane offsets of that step
+  // the load cursor: step l_step (l_off bytes on) of the sequence's tile l_it, whose coordinates are (l_m, l_n); the
+  // lane offsets of that step
   u32x4 ad{}, wd{};
-  int l_it = 0, l_step = 0;
-  int a_at[2], w_at[2];
+  int l_it = 0, l_step = 0, l_off = 0, l_m = 0, l_n = 0;
+  int a_at[2], w_at[4];
   auto set_tile = [&](int it) {
     if (it < seq.count) {
-      int tm, tn;
-      seq.coords(it, tm, tn);
-      ad = make_desc(A + (int64_t)tm * BM * lda, min((int64_t)0x7FFFFFFF, (int64_t)(M - tm * BM - 1) * lda + K));
-      wd = make_desc(W + (int64_t)tn * BN * ldw, min((int64_t)0x7FFFFFFF, (int64_t)(N - tn * BN - 1) * ldw + K));
+      seq.coords(it, l_m, l_n);
+      ad = make_desc(A + (int64_t)l_m * BM * lda, min((int64_t)0x7FFFFFFF, (int64_t)(M - l_m * BM - 1) * lda + K));
+      wd = make_desc(W + (int64_t)l_n * BN * ldw, min((int64_t)0x7FFFFFFF, (int64_t)(N - l_n * BN - 1) * ldw + K));
     } else {   // past the last tile: empty ranges
       ad[2] = 0;
       wd[2] = 0;
     }
   };
+  // only a tile's last step differs from the others.  (The lane is hidden from
+  // the compiler here and in the epilogue: it would form what depends on it once,
+  // before the tiles, and keep that in scratch memory.)
   auto set_step = [&] {
-    const int last = l_step == KT - 1 ? -1 : 0;
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int live = l_step == KT - 1 ? tail_chunks : 8;   // chunks of this step; offsets of rows are below 2^30
 #pragma unroll
-    for (int par = 0; par < 2; ++par) {   // offsets of rows are below 2^30
-      a_at[par] = a_vo[par] | (behind[par] & last);
-      w_at[par] = w_vo[par] | (behind[par] & last);
+    for (int u = 0; u < 2; ++u) {
+      const int c = (ln & 7) ^ row_swizzle(8 * (LA * wave + u) + (ln >> 3));
+      a_at[u] = ((LA * wave * 8 + (ln >> 3)) * (int)lda + c * 16) | (c < live ? 0 : (int)kNowhere);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int c = (ln & 7) ^ channel_swizzle(8 * (LW * wave + u) + (ln >> 3));
+      w_at[u] = ((LW * wave * 8 + (ln >> 3)) * (int)ldw + c * 16) | (c < live ? 0 : (int)kNowhere);
     }
   };
   auto advance = [&] {
-    if (++l_step == KT) {
-      l_step = 0;
-      set_tile(++l_it);
+    l_off += BK;
+    if (++l_step >= KT - 1) {
+      if (l_step == KT) {
+        l_step = l_off = 0;
+        set_tile(++l_it);
+      }
+      if (tail_chunks < 8) set_step();
     }
-    set_step();
   };
-  auto load_a = [&](int u, int slot) {
-    load_lds16(ad, a_at[u & 1] + u * a_pc, l_step * BK, lds_base + slot * S::kSlotA + (LA * wave + u) * 1024);
-  };
-  auto load_w = [&](int u, int slot) {
-    load_lds16(wd, w_at[u & 1] + u * w_pc, l_step * BK, lds_base + S::kBaseW + slot * S::kSlotW + (LW * wave + u) * 1024);
-  };
-  auto load_x = [&](int u, int slot) { if (XA) load_a(u, slot); else load_w(u, slot); };
-  auto load_y = [&](int u, int slot) { if (XA) load_w(u, slot); else load_a(u, slot); };
+  const uint32_t lds_a = lds_base + LA * 1024 * wave, lds_w = lds_base + S::kBaseW + LW * 1024 * wave;
+  constexpr int SX = XA ? S::kSlotA : S::kSlotW, SY = XA ? S::kSlotW : S::kSlotA;   // bytes of a slot
+  const uint32_t lds_x = XA ? lds_a : lds_w, lds_y = XA ? lds_w : lds_a;
 
-  // ---- fragment reads: row base + 16 b + (lane & 15), logical chunk 4 kk + (lane >> 4) of half kk
+  // ---- fragment reads: logical chunk 4 kk + (lane >> 4) of half kk; of A, row
+  // base + 16 b + (lane & 15); of W, the rows that make block pair k of a lane's
+  // results eight channels in a row: block 2 k + h takes, as its rows 4 f + e,
+  // the channels 32 k + 8 f + 4 h + e.
+  static_assert(NB % 2 == 0, "blocks of W come in pairs");
   const int fr = lane & 15, fh = lane >> 4;
-  const int sw = row_swizzle(fr);   // == row_swizzle(base + 16 b + fr)
-  int fo_a[2], fo_w[2];             // + 16 * kRowBytes b
+  const int wrow = wn * 16 * NB + 8 * (fr >> 2) + (fr & 3);
+  int fo_a[2], fo_w[2];             // + 16 * kRowBytes b, + w_block(i)
 #pragma unroll
   for (int kk = 0; kk < 2; ++kk) {
-    fo_a[kk] = (wm * 16 * MB + fr) * kRowBytes + (((4 * kk + fh) ^ sw) << 4);
-    fo_w[kk] = S::kBaseW + (wn * 16 * NB + fr) * kRowBytes + (((4 * kk + fh) ^ sw) << 4);
+    fo_a[kk] = (wm * 16 * MB + fr) * kRowBytes + (((4 * kk + fh) ^ row_swizzle(fr)) << 4);   // the swizzles of all blocks' rows
+    fo_w[kk] = S::kBaseW + wrow * kRowBytes + (((4 * kk + fh) ^ channel_swizzle(wrow)) << 4);
   }
+  auto w_block = [](int i) { return (32 * (i >> 1) + 4 * (i & 1)) * kRowBytes; };
   struct Frags { i32x4 w[NB], a[MB]; };
   Frags f0, f1;
-  // acc[i][j][e] = sum of row m, column n, m = 16 MB wm + 16 j + fr and n = 16 NB wn + 16 i + 4 fh + e of the tile
+
+  // ---- the scales and biases of a tile: the wave's own go into the part of the
+  // last step's Y slot that the wave itself refills in the next step, from byte 0
+  // (rows), 512 (channels) and 1024 (biases) of it on; behind the last they are zeros.
+  auto scales_at = [&](int py) { return (XA ? S::kBaseW : 0) + py + wave * (LY * 1024); };
+  auto load_scales = [&](int m0, int n0, int py) {
+    const int m = m0 + wm * 16 * MB, n = n0 + wn * 16 * NB;
+    const uint32_t to = lds_base + scales_at(py);
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const u32x4 ds = make_desc(ep.sa + m, (int64_t)(M - m) * 4), dw = make_desc(ep.sw + n, (int64_t)(N - n) * 4);
+    const u32x4 db = make_desc(ep.bias + n, ep.bias ? (int64_t)(N - n) * (int)sizeof(T) : 0);
+#pragma unroll
+    for (int q = 0; q < (16 * MB + 63) / 64; ++q) load_lds_4(ds, 4 * ln + 256 * q, to + 256 * q);
+#pragma unroll
+    for (int q = 0; q < (16 * NB + 63) / 64; ++q) load_lds_4(dw, 4 * ln + 256 * q, to + 512 + 256 * q);
+#pragma unroll
+    for (int q = 0; q < (16 * NB * (int)sizeof(T) + 255) / 256; ++q) load_lds_4(db, 4 * ln + 256 * q, to + 1024 + 256 * q);
+  };
+  static_assert(LY >= 4, "the scales fit");
+  // acc[2 k + h][j][e] = sum of row m, channel n of the tile, m = 16 MB wm + 16 j + fr, n = 16 NB wn + 32 k + 8 fh + 4 h + e
   i32x4 acc[NB][MB];
 
-  // One half: the MFMAs on f, each followed by its share of the reads of the
-  // next half into g and of the loads, fenced so that the compiler keeps this order.
+  // One half: the MFMAs on f, among them the reads of the next half's fragments
+  // into g (from ra and rw on) and the loads of X or Y into the slot at lds,
+  // fenced so that the compiler keeps this order.  A wave issues an instruction
+  // every 4 cycles and an MFMA takes 16, so at most three others go between two
+  // MFMAs.  The reads are in the order of their use, w0, a0 .., w1 ..; before
+  // the barrier (X: false) they end early, so that they have landed there.
   constexpr int NM = MB * NB, NR = MB + NB;
-  constexpr int kReadStep = 2, kLoadStep = NM >= 48 ? 4 : 2;
-  static_assert((NM - 1) / kReadStep + 1 >= NR && (NM - 1) / kLoadStep + 1 >= (LX > LY ? LX : LY), "all reads and loads are issued");
-  auto half = [&](const Frags& f, Frags& g, int slot_x, int slot_y, int kk, auto loads_x, int load_slot) __attribute__((always_inline)) {
-    constexpr bool kX = decltype(loads_x)::value;
-    const char* const pa = smem + (XA ? slot_x : slot_y) * S::kSlotA + fo_a[kk];
-    const char* const pw = smem + (XA ? slot_y : slot_x) * S::kSlotW + fo_w[kk];
+  auto half = [&](const Frags& f, Frags& g, int ra, int rw, uint32_t lds, auto loads_x, auto first) __attribute__((always_inline)) {
+    constexpr bool kX = decltype(loads_x)::value, kA = kX == XA;   // kA: the loads are A's
+    constexpr int kReadStep = NM >= 64 ? (kX ? 4 : 3) : NM >= 48 && kX ? 3 : 2, kLoads = kX ? LX : LY;
+    static_assert((NM - 1) / kReadStep + 1 >= NR && 4 * kLoads <= NM, "all reads and loads are issued");
+    int vo[8];
+    auto prepare = [&](auto at) __attribute__((always_inline)) {
+      constexpr int u = decltype(at)::value;
+      vo[u] = kA ? a_at[u & 1] + u * a_pc : w_at[u & 3] + u * w_pc;
+      load_lds_to<u * 1024>(lds, vo[u]);
+    };
 #pragma unroll
     for (int m = 0; m < NM; ++m) {
       const int i = m / MB, j = m % MB;
-      mfma16(acc[i][j], f.w[i], f.a[j]);
-      const int r = m / kReadStep;   // reads in the order of their use: w0, a0 .., w1 ..
+      if (decltype(first)::value) mfma16_first(acc[i][j], f.w[i], f.a[j]);
+      else mfma16(acc[i][j], f.w[i], f.a[j]);
+      const int r = m / kReadStep;
       if (m % kReadStep == 0 && r < NR) {
-        if (r == 0) g.w[0] = *reinterpret_cast<const i32x4*>(pw);
-        else if (r <= MB) g.a[r - 1] = *reinterpret_cast<const i32x4*>(pa + (r - 1) * 16 * kRowBytes);
-        else g.w[r - MB] = *reinterpret_cast<const i32x4*>(pw + (r - MB) * 16 * kRowBytes);
+        if (r == 0) g.w[0] = *reinterpret_cast<const i32x4*>(smem + rw);
+        else if (r <= MB) g.a[r - 1] = *reinterpret_cast<const i32x4*>(smem + ra + (r - 1) * 16 * kRowBytes);
+        else g.w[r - MB] = *reinterpret_cast<const i32x4*>(smem + rw + w_block(r - MB));
       }
-      const int l = m / kLoadStep;
-      if (m % kLoadStep == 0 && l < (kX ? LX : LY)) {
-        if (kX) load_x(l, load_slot);
-        else load_y(l, load_slot);
+      const int l = m / 4;
+      if (m % 4 == 1 && l < kLoads) {
+        switch (l) {   // the index as a constant of the assembly
+          case 0: prepare(std::integral_constant<int, 0>{}); break;
+          case 1: prepare(std::integral_constant<int, 1>{}); break;
+          case 2: prepare(std::integral_constant<int, 2>{}); break;
+          case 3: prepare(std::integral_constant<int, 3>{}); break;
+          case 4: prepare(std::integral_constant<int, 4>{}); break;
+          case 5: prepare(std::integral_constant<int, 5>{}); break;
+          case 6: prepare(std::integral_constant<int, 6>{}); break;
+          default: prepare(std::integral_constant<int, 7>{}); break;
+        }
       }
+      if (m % 4 == 3 && l < kLoads) load_lds_16(kA ? ad : wd, vo[l], l_off);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -178,176 +255,164 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
 #pragma unroll
   for (int s = 0; s < RX; ++s) {
 #pragma unroll
-    for (int u = 0; u < LX; ++u) load_x(u, s);
+    for (int u = 0; u < LA; ++u) load_lds16(ad, a_at[u & 1] + u * a_pc, l_off, lds_a + s * S::kSlotA + u * 1024);
 #pragma unroll
-    for (int u = 0; u < LY; ++u) load_y(u, s);
+    for (int u = 0; u < LW; ++u) load_lds16(wd, w_at[u & 3] + u * w_pc, l_off, lds_w + s * S::kSlotW + u * 1024);
     advance();
   }
   wait_vmcnt<(RX - 1) * (LX + LY)>();
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < NB; ++i) f0.w[i] = *reinterpret_cast<const i32x4*>(smem + fo_w[0] + i * 16 * kRowBytes);
+  for (int i = 0; i < NB; ++i) f0.w[i] = *reinterpret_cast<const i32x4*>(smem + fo_w[0] + w_block(i));
 #pragma unroll
   for (int j = 0; j < MB; ++j) f0.a[j] = *reinterpret_cast<const i32x4*>(smem + fo_a[0] + j * 16 * kRowBytes);
-  int sx = 0, sy = 0;   // slots of the current step, counted over all tiles: mod RX, mod RY
+  // slots of the current step, counted over all tiles, as bytes into the rings; tile coordinates as the cursor found them
+  int px = 0, py = 0;
+  auto next_x = [](int p) { return p == (RX - 1) * SX ? 0 : p + SX; };
+  auto next_y = [](int p) { return p == (RY - 1) * SY ? 0 : p + SY; };
+  auto last_y = [](int p) { return p == 0 ? (RY - 1) * SY : p - SY; };
+  constexpr int kStores = MB * NB / 2;                       // of a wave's epilogue
+  constexpr int kPending = (RX - 2) * LX + (RX - 1) * LY;    // loads that may be in flight at a step's barrier
+  static_assert(kPending + kStores <= 63, "the counter's range");
   for (int it = 0; it < seq.count; ++it) {
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-      for (int j = 0; j < MB; ++j) acc[i][j] = i32x4{};
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_nop 1");   // a vector write of an MFMA's addend
-    __builtin_amdgcn_sched_barrier(0);
-    int tm, tn;
-    seq.coords(it, tm, tn);
+    int tm = l_m, tn = l_n;   // the load cursor is in this tile, or, with few steps a tile, further on
+    if (KT <= RX) seq.coords(it, tm, tn);
     const int m0 = tm * BM, n0 = tn * BN;
-    int last_y = 0;
-    for (int s = 0; s < KT; ++s) {
-      const int sx1 = sx == RX - 1 ? 0 : sx + 1;
-      const int sy1 = sy == RY - 1 ? 0 : sy + 1;
-      half(f0, f1, sx, sy, 1, std::false_type{}, sy == 0 ? RY - 1 : sy - 1);   // loads Y(s + R) into the slot of s - 1
-      // X(s + 1) and Y(s + 1) have landed; R - 2 steps of X and R - 1 of Y may still be in flight
-      wait_vmcnt<(RX - 2) * LX + (RX - 1) * LY>();
+    // A step's first half loads Y(s + R) into the slot of s - 1.  Then X(s + 1)
+    // and Y(s + 1) have to have landed; R - 2 steps of X and R - 1 of Y may still
+    // be in flight and, in a tile's first step, the stores of the tile before.
+    half(f0, f1, fo_a[1] + (XA ? px : py), fo_w[1] + (XA ? py : px), lds_y + last_y(py), std::false_type{}, std::true_type{});
+    if (it == 0) wait_vmcnt<kPending>();
+    else wait_vmcnt<kPending + kStores>();
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+    for (int s = 0;;) {
+      const int px1 = next_x(px), py1 = next_y(py);
+      if (s == KT - 1) load_scales(m0, n0, py);
+      // the second half loads X(s + R) into the slot of s
+      half(f1, f0, fo_a[0] + (XA ? px1 : py1), fo_w[0] + (XA ? py1 : px1), lds_x + px, std::true_type{}, std::false_type{});
+      advance();
+      if (++s == KT) break;
+      px = px1;
+      py = py1;
+      half(f0, f1, fo_a[1] + (XA ? px : py), fo_w[1] + (XA ? py : px), lds_y + last_y(py), std::false_type{}, std::false_type{});
+      wait_vmcnt<kPending>();
       __syncthreads();
       __builtin_amdgcn_sched_barrier(0);
-      half(f1, f0, sx1, sy1, 0, std::true_type{}, sx);                         // loads X(s + R) into the slot of s
-      advance();
-      last_y = sy;
-      sx = sx1;
-      sy = sy1;
     }
-    // wait states from the last MFMA to a vector read of its result (the compiler itself would put at most 12)
+    // wait states from the last MFMA to a vector read of its result (the
+    // compiler itself would put at most 12), and the scales, which only the last
+    // step's X loads follow
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_nop 15" ::: "memory");
+    wait_vmcnt<LX>();
     __builtin_amdgcn_sched_barrier(0);
 
-    // Epilogue through a wave-private LDS window of 32 rows x CW columns
-    // (fp32), in the part of the last step's Y slot that this wave itself
-    // refills in the next step: the places, permutation and swizzle of the
-    // bf16 kernel's.  What goes through the window is the sum times the row's
-    // scale, which a lane of the MFMA layout needs one of per block.  One
-    // wave's LDS operations complete in order, so the window needs no barrier.
-    // out may be res: every element is read before it is written, by the same lane.
-    constexpr int CW = NB % 4 == 0 && LY >= 8 ? 64 : 32;   // the wave's share of a Y slot is LY KiB
-    constexpr int LPR = CW / 8, RPP = 64 / LPR;            // lanes per row and rows per pass when read back
-    constexpr int NP = 32 / RPP, NV = NB * 16 / CW;        // passes per window, windows per row block pair
-    static_assert(32 * CW * 4 <= LY * 1024 && NB * 16 % CW == 0 && MB % 2 == 0, "the window fits");
+    // Epilogue, straight from the accumulators: a lane holds eight channels in a
+    // row of each block pair and row, so a wave's store is 16 rows x 64 bytes.
+    // Rows behind the last are behind the descriptor's end, channels behind the
+    // last at an offset that it does not reach: every wave issues all its stores,
+    // which the next tile's first wait counts on.  out may be res: every element
+    // is read before it is written, by the same lane.
     constexpr bool kRes = EPI == DIT_EPI_RESIDUAL || EPI == DIT_EPI_GATED_RESIDUAL;
-    constexpr int kAhead = sizeof(T) == 2 ? 1 : 0;         // row block pairs by which the residual is loaded ahead
-    char* const ew = smem + (XA ? S::kBaseW + last_y * S::kSlotW : last_y * S::kSlotA) + wave * (LY * 1024);
-    // The lane, hidden from the compiler: it would form the window's addresses
-    // once before the tiles, and keep them in scratch memory meanwhile.
+    constexpr int NP = NB / 2, ES = sizeof(T);
+    constexpr int kAhead = ES == 2 ? 1 : 0;   // row blocks by which the residual is loaded ahead
+    const int mw = m0 + wm * 16 * MB, nw = n0 + wn * 16 * NB;   // the wave's first row and channel
     int el = lane;
     asm volatile("" : "+v"(el));
-    const int er = el / LPR, ec = el % LPR, wr = el & 15, wh = el >> 4;
-    auto at = [](int r, int c) {   // LDS byte of chunk c of window row r
-      if (CW == 64) return r * 256 + ((((c >> 1) | ((c & 1) << 3)) ^ (((r & 1) << 3) | ((r >> 1) & 7))) << 4);
-      return r * 128 + ((((c >> 1) | ((c & 1) << 2)) ^ ((((r >> 1) & 1) << 2) | ((r >> 2) & 3))) << 4);
-    };
-    const int nw = n0 + wn * 16 * NB + 8 * ec;   // the lane's first column of window 0
-    float row_scale[MB];
+    const int er = el & 15, eh = el >> 4;
+    const char* const sc = smem + scales_at(py);
+    float wscale[NP][8], bias[NP][8];
+    float row_scale[2];   // of this row block and the next
+    row_scale[0] = *reinterpret_cast<const float*>(sc + 4 * er);
 #pragma unroll
-    for (int j = 0; j < MB; ++j) row_scale[j] = ep.sa[min(m0 + wm * 16 * MB + 16 * j + wr, M - 1)];
-    float wscale[NV][8], bsum[NV][8];
+    for (int k = 0; k < NP; ++k) {
+      const f32x4* const w4 = reinterpret_cast<const f32x4*>(sc + 512 + 4 * (32 * k + 8 * eh));
+      const V8 b8 = *reinterpret_cast<const V8*>(sc + 1024 + ES * (32 * k + 8 * eh));
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int n = nw + CW * v;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) wscale[v][e] = bsum[v][e] = 0.f;
-      if (n < N) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) wscale[v][e] = ep.sw[n + e];
-        if (ep.bias) {
-          const V8 bv = *reinterpret_cast<const V8*>(ep.bias + n);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) bsum[v][e] = (float)bv[e];
-        }
+      for (int e = 0; e < 8; ++e) {
+        wscale[k][e] = w4[e / 4][e % 4];
+        bias[k][e] = (float)b8[e];
       }
     }
-    V8 rv[1 + kAhead][NV][NP];
+    int out_at[NP], res_at[NP];   // lane offsets inside 16 rows
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      const bool in = nw + 8 * eh + 32 * k < N;
+      out_at[k] = in ? (er * (int)ep.ldo + 8 * eh) * ES : (int)kNowhere;
+      res_at[k] = kRes && in ? (er * (int)ep.ldr + 8 * eh) * ES : (int)kNowhere;
+    }
+    auto rows_of = [&](const T* p, int64_t ld, int j) {   // the wave's rows 16 j .. 16 j + 15 from its first channel on
+      const int m = mw + 16 * j;
+      return __builtin_amdgcn_make_buffer_rsrc((void*)(p + (int64_t)m * ld + nw), 0, m < M ? min(16, M - m) * (int)ld * ES : 0,
+                                               0x00020000);
+    };
+    f32x4 rv[1 + kAhead][NP][ES / 2];
     auto load_res = [&](int j) __attribute__((always_inline)) {
       if constexpr (kRes) {
+        const auto d = rows_of(ep.res, ep.ldr, j);
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int k = 0; k < NP; ++k)
 #pragma unroll
-          for (int p = 0; p < NP; ++p) {
-            const int m = m0 + wm * 16 * MB + 32 * j + RPP * p + er, n = nw + CW * v;
-            rv[j & kAhead][v][p] = V8{};
-            if (m < M && n < N) rv[j & kAhead][v][p] = *reinterpret_cast<const V8*>(ep.res + (int64_t)m * ep.ldr + n);
-          }
+          for (int q = 0; q < ES / 2; ++q)
+            rv[j & kAhead][k][q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(d, res_at[k] + 32 * ES * k + 16 * q, 0, 0));
       }
     };
     if (kAhead) load_res(0);
+    f32x4 gv[NP][2];
+    bool g_one = true;   // all rows of the wave belong to one request
+    auto load_gate = [&](int r) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < MB / 2; ++j) {
-      if (j + kAhead < MB / 2) load_res(j + kAhead);
-      const int mb = m0 + wm * 16 * MB + 32 * j;   // first row of the pair
-      f32x4 gv[NV][2];
-      bool g_one = true;                           // all rows of the pair belong to one request
-      if (EPI == DIT_EPI_GATED_RESIDUAL) {
-        const int r_lo = find_req(ep.req.cu, ep.req.n_req, min(mb, M - 1));
-        const int r_hi = find_req(ep.req.cu, ep.req.n_req, min(mb + 31, M - 1));
-        g_one = r_lo == r_hi;
+      for (int k = 0; k < NP; ++k) {
+        const float* const gp = ep.gate + (int64_t)r * ep.gate_stride + min(nw + 32 * k + 8 * eh, N - 8);
+        gv[k][0] = *reinterpret_cast<const f32x4*>(gp);
+        gv[k][1] = *reinterpret_cast<const f32x4*>(gp + 4);
+      }
+    };
+    if constexpr (EPI == DIT_EPI_GATED_RESIDUAL) {
+      const int r = find_req(ep.req.cu, ep.req.n_req, min(mw, M - 1));
+      g_one = r == find_req(ep.req.cu, ep.req.n_req, min(mw + 16 * MB - 1, M - 1));
+      load_gate(r);
+    }
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          gv[v][0] = gv[v][1] = f32x4{};
-          if (g_one && nw + CW * v < N) {
-            const float* gp = ep.gate + (int64_t)r_lo * ep.gate_stride + nw + CW * v;
-            gv[v][0] = *reinterpret_cast<const f32x4*>(gp);
-            gv[v][1] = *reinterpret_cast<const f32x4*>(gp + 4);
+    for (int j = 0; j < MB; ++j) {
+      if (j + 1 < MB) row_scale[(j + 1) & 1] = *reinterpret_cast<const float*>(sc + 4 * (16 * (j + 1) + er));
+      if (j + kAhead < MB) load_res(j + kAhead);
+      if (EPI == DIT_EPI_GATED_RESIDUAL && !g_one) load_gate(find_req(ep.req.cu, ep.req.n_req, min(mw + 16 * j + er, M - 1)));
+      const auto d = rows_of(ep.out, ep.ldo, j);
+#pragma unroll
+      for (int k = 0; k < NP; ++k) {
+        __builtin_amdgcn_sched_barrier(0);   // more of them in flight cost spilled registers
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = fmaf((float)sum_of(acc[2 * k + e / 4][j], e % 4) * row_scale[j & 1], wscale[k][e], bias[k][e]);
+        if constexpr (EPI == DIT_EPI_GELU_TANH) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) z[e] = gelu_tanh(z[e]);
+        } else if constexpr (kRes) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float r = ES == 2 ? (float)__builtin_bit_cast(bf16x8, rv[j & kAhead][k][0])[e] : rv[j & kAhead][k][e / 4 % (ES / 2)][e % 4];
+            z[e] = EPI == DIT_EPI_GATED_RESIDUAL ? fmaf(gv[k][e / 4][e % 4], z[e], r) : r + z[e];
           }
         }
-      }
+        if constexpr (ES == 2) {
+          u32x4 o;
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
+          for (int e = 0; e < 4; ++e) o[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{z[2 * e], z[2 * e + 1]}, bf16x2));
+          __builtin_amdgcn_raw_buffer_store_b128(o, d, out_at[k] + 64 * k, 0, 0);
+        } else {
 #pragma unroll
-        for (int ii = 0; ii < CW / 16; ++ii)
-#pragma unroll
-          for (int jj = 0; jj < 2; ++jj) {
-            const i32x4 c = acc[v * (CW / 16) + ii][2 * j + jj];
-            f32x4 z;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] = (float)c[e] * row_scale[2 * j + jj];
-            *reinterpret_cast<f32x4*>(ew + at(16 * jj + wr, 4 * ii + wh)) = z;
-          }
-        const int n = nw + CW * v;
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const int r = RPP * p + er, m = mb + r;
-          const f32x4 z0 = *reinterpret_cast<const f32x4*>(ew + at(r, 2 * ec));
-          const f32x4 z1 = *reinterpret_cast<const f32x4*>(ew + at(r, 2 * ec + 1));
-          float z[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) z[e] = fmaf(e < 4 ? z0[e & 3] : z1[e & 3], wscale[v][e], bsum[v][e]);
-          if (EPI == DIT_EPI_GELU_TANH) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = gelu_tanh(z[e]);
-          } else if (EPI == DIT_EPI_GATED_RESIDUAL) {
-            f32x4 g0 = gv[v][0], g1 = gv[v][1];
-            if (!g_one && m < M && n < N) {   // the pair spans a request boundary
-              const float* gp = ep.gate + (int64_t)find_req(ep.req.cu, ep.req.n_req, m) * ep.gate_stride + n;
-              g0 = *reinterpret_cast<const f32x4*>(gp);
-              g1 = *reinterpret_cast<const f32x4*>(gp + 4);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = fmaf(e < 4 ? g0[e & 3] : g1[e & 3], z[e], (float)rv[j & kAhead][v][p][e]);
-          } else if (EPI == DIT_EPI_RESIDUAL) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = (float)rv[j & kAhead][v][p][e] + z[e];
-          }
-          V8 o;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = (T)z[e];
-          // computed on every path: were it left to the branch, a load above
-          // would be pending where the branch is not taken, and the compiler
-          // would wait for all loads in the K loop
-          asm volatile("" : "+v"(o));
-          if (m < M && n < N) *reinterpret_cast<V8*>(ep.out + (int64_t)m * ep.ldo + n) = o;
+          for (int q = 0; q < 2; ++q)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{z[4 * q], z[4 * q + 1], z[4 * q + 2], z[4 * q + 3]}), d,
+                                                   out_at[k] + 128 * k + 16 * q, 0, 0);
         }
       }
     }
-    // the window's reads are done before the next step's loads overwrite it
+    // the scales are read before the next step's loads overwrite them, and no store moves behind those loads
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    px = next_x(px);
+    py = next_y(py);
   }
   wait_vmcnt<0>();   // no load may land in LDS after the workgroup has ended
 }
@@ -466,13 +531,12 @@ constexpr TileCost kCost[5] = {
     {128, 192, 3.34f, 0.4396f, 0.1457f}, {128, 128, 2.74f, 0.3213f, 0.1101f}};
 constexpr int kFew = 5;   // the index of the kernel for few rows
 constexpr int kFewRows = 64;
-constexpr int kFewColumns = 1 << 24;   // 512 work-items for 16 channels: 2^29 in the launch's first dimension
 int few_tile_m(int64_t M) { return M <= 16 ? 16 : M <= 32 ? 32 : 64; }
 
 std::atomic<int> g_shape{-1};   // forced shape (-1: chosen per call)
 
 int choose(int64_t M, int N, int K, int cus) {
-  const bool few = M <= 64 * kFewRows && N <= kFewColumns;   // what the launch of that kernel holds
+  const bool few = M <= 64 * kFewRows;   // what that kernel is launched with
   const int forced = g_shape.load(std::memory_order_relaxed);
   if (forced >= 0 && (forced != kFew || few)) return forced;
   if (few && M <= kFewRows) return kFew;

@@ -47,10 +47,28 @@ def test_accumulators_keep_their_distance(kernels):
 
 
 def test_k_loop_has_no_copies_and_no_full_waits(kernels):
+    """The halves of a step (and a tile's first half): no copies of accumulators, no spills, one wait for loads."""
     for name, body in kernels.items():
-        loops = [b for b in _blocks(body) if sum("v_mfma" in l for _, l, _ in b["ins"]) >= 32]
-        assert len(loops) == 1, name
-        ins = [l for _, l, _ in loops[0]["ins"]]
-        assert not [l for l in ins if l.startswith(("v_accvgpr", "scratch_", "v_readlane", "v_writelane"))], name
+        assert not [l for l in body if "scratch_" in l], name
+        halves = [b for b in _blocks(body) if any("v_mfma" in l for _, l, _ in b["ins"])]
+        assert len(halves) == 3, name
+        ins = [l for b in halves for _, l, _ in b["ins"]]
+        assert not [l for l in ins if l.startswith(("v_accvgpr", "v_readlane", "v_writelane"))], name
         waits = [int(m.group(1)) for l in ins for m in re.finditer(r"vmcnt\((\d+)\)", l)]
         assert len(waits) == 1 and waits[0] >= 6, f"{name}: vmcnt waits {waits}"
+
+
+def test_the_lds_address_of_a_load_is_the_one_set_for_it(kernels):
+    """Between the instruction that sets m0 and its load, which are separate statements, nothing else writes m0."""
+    for name, body in kernels.items():
+        writer, loads = None, 0
+        for l in body:
+            l = l.strip()
+            if re.match(r"s_\w+ m0\b", l):
+                writer = l
+            elif l.startswith(("s_", "v_")) and re.search(r"\bm0\b", l.split(",")[0]):
+                raise AssertionError(f"{name}: {l}")
+            elif l.startswith("buffer_load") and l.endswith("lds"):
+                assert writer is not None, f"{name}: {l} without its own address"
+                writer, loads = None, loads + 1
+        assert loads > 8, name

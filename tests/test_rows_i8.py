@@ -118,6 +118,9 @@ def linear(L, a=X, lda=64, sa=SC, w=W, ldw=64, sw=WS, bias=G, out=O, ldo=64, M=4
     (linear, dict(lda=48), BAD, b"lda"),
     (linear, dict(ldw=72), BAD, b"lda"),
     (linear, dict(lda=(1 << 22) + 16), BAD, b"lda"),
+    (linear, dict(N=(1 << 24) + 8, ldo=1 << 25), NOT, b"N <="),
+    (linear, dict(ldo=(1 << 24) + 8), BAD, b"ldo"),
+    (linear, dict(epi=B.EPI_RESIDUAL, ldr=(1 << 24) + 8), BAD, b"ldr"),
     (linear, dict(ldo=56), BAD, b"ldo"),
     (linear, dict(ldo=68), BAD, b"ldo"),
     (linear, dict(epi=B.EPI_RESIDUAL, ldr=56), BAD, b"ldr"),
@@ -224,7 +227,6 @@ def plan(L, M, N, K, cus=256):
 
 def test_the_choice_of_tiles(L):
     assert plan(L, 1, 5120, 5120) == (16, 16) and plan(L, 17, 5120, 5120) == (32, 16)
-    assert plan(L, 1, 1 << 25, 16)[1] > 16              # more channels than that kernel's launch holds
     assert plan(L, 75600, 15360, 5120) == (256, 256)
     m, n = ctypes.c_int(), ctypes.c_int()
     f = L.dit_debug_linear_i8_plan
