@@ -72,6 +72,37 @@ struct Epi {
   ReqTable req;
 };
 
+// The tiles of a workgroup in tile_seq's order, one after the other without a
+// division by a variable per tile: place r of its raster group, whose rows are g
+// (below 2^5; r is below 2^27, where r inv >> 32 is r / g).
+struct TileWalk {
+  int left, r, first_m, g, stride, tiles_m, tiles_n, group_m;
+  uint32_t inv;   // ceil(2^32 / g)
+  __device__ void group(int m) {
+    first_m = m;
+    g = min(tiles_m - m, group_m);
+    inv = g > 1 ? 0xFFFFFFFFu / (uint32_t)g + 1 : 0;
+  }
+  __device__ explicit TileWalk(const TileSeq& q)
+      : left(q.count), stride(q.stride), tiles_m(q.tiles_m), tiles_n(q.tiles_n), group_m(q.group_m) {
+    const int width = group_m * tiles_n;
+    r = q.first % width;
+    group(q.first / width * group_m);
+  }
+  __device__ bool next(int& tm, int& tn) {   // false: none is left
+    if (left == 0) return false;
+    --left;
+    while (__builtin_expect(r >= g * tiles_n, 0)) {   // on in a later group
+      r -= g * tiles_n;
+      group(first_m + g);
+    }
+    tn = g > 1 ? (int)(((uint64_t)(uint32_t)r * inv) >> 32) : r;
+    tm = first_m + r - tn * g;
+    r += stride;
+    return true;
+  }
+};
+
 // ------------------------------------------------------------------- tiles
 //
 // The scheme of the bf16 kernel: a workgroup per compute unit takes a sequence
@@ -102,6 +133,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
 
   const TileSeq seq = tile_seq(blockIdx.x, gridDim.x, tiles_m, tiles_n, group_m);
   if (seq.count == 0) return;
+  TileWalk walk(seq);
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -117,14 +149,13 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
   static_assert(LA % 2 == 0 && LW % 2 == 0, "the parity of a piece is that of its index in the wave");
   const int a_pc = 8 * (int)lda, w_pc = 8 * (int)ldw;   // bytes of 8 rows
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  // the load cursor: step l_step (l_off bytes on) of the sequence's tile l_it, whose coordinates are (l_m, l_n); the
-  // lane offsets of that step
+  // the load cursor: step l_step (l_off bytes on) of its tile, whose coordinates are (l_m, l_n); the lane offsets of that
+  // step
   u32x4 ad{}, wd{};
-  int l_it = 0, l_step = 0, l_off = 0, l_m = 0, l_n = 0;
+  int l_step = 0, l_off = 0, l_m = 0, l_n = 0;
   int a_at[2], w_at[4];
-  auto set_tile = [&](int it) {
-    if (it < seq.count) {
-      seq.coords(it, l_m, l_n);
+  auto set_tile = [&]() __attribute__((always_inline)) {
+    if (walk.next(l_m, l_n)) {
       ad = make_desc(A + (int64_t)l_m * BM * lda, min((int64_t)0x7FFFFFFF, (int64_t)(M - l_m * BM - 1) * lda + K));
       wd = make_desc(W + (int64_t)l_n * BN * ldw, min((int64_t)0x7FFFFFFF, (int64_t)(N - l_n * BN - 1) * ldw + K));
     } else {   // past the last tile: empty ranges
@@ -135,7 +166,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
   // only a tile's last step differs from the others.  (The lane is hidden from
   // the compiler here and in the epilogue: it would form what depends on it once,
   // before the tiles, and keep that in scratch memory.)
-  auto set_step = [&] {
+  auto set_step = [&]() __attribute__((always_inline)) {
     int ln = lane;
     asm volatile("" : "+v"(ln));
     const int live = l_step == KT - 1 ? tail_chunks : 8;   // chunks of this step; offsets of rows are below 2^30
@@ -150,12 +181,12 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
       w_at[u] = ((LW * wave * 8 + (ln >> 3)) * (int)ldw + c * 16) | (c < live ? 0 : (int)kNowhere);
     }
   };
-  auto advance = [&] {
+  auto advance = [&]() __attribute__((always_inline)) {
     l_off += BK;
-    if (++l_step >= KT - 1) {
+    if (__builtin_expect(++l_step >= KT - 1, 0)) {
       if (l_step == KT) {
         l_step = l_off = 0;
-        set_tile(++l_it);
+        set_tile();
       }
       if (tail_chunks < 8) set_step();
     }
@@ -185,19 +216,19 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
   // last step's Y slot that the wave itself refills in the next step, from byte 0
   // (rows), 512 (channels) and 1024 (biases) of it on; behind the last they are zeros.
   auto scales_at = [&](int py) { return (XA ? S::kBaseW : 0) + py + wave * (LY * 1024); };
-  auto load_scales = [&](int m0, int n0, int py) {
-    const int m = m0 + wm * 16 * MB, n = n0 + wn * 16 * NB;
-    const uint32_t to = lds_base + scales_at(py);
+  const u32x4 sa_d = make_desc(ep.sa, (int64_t)M * 4), sw_d = make_desc(ep.sw, (int64_t)N * 4);
+  const u32x4 bias_d = make_desc(ep.bias, ep.bias ? (int64_t)N * (int)sizeof(T) : 0);
+  auto load_scales = [&](int m0, int n0, int at) __attribute__((always_inline)) {
+    const uint32_t to = lds_base + at;
     int ln = lane;
     asm volatile("" : "+v"(ln));
-    const u32x4 ds = make_desc(ep.sa + m, (int64_t)(M - m) * 4), dw = make_desc(ep.sw + n, (int64_t)(N - n) * 4);
-    const u32x4 db = make_desc(ep.bias + n, ep.bias ? (int64_t)(N - n) * (int)sizeof(T) : 0);
+    const int m = 4 * (m0 + wm * 16 * MB + ln), n = 4 * (n0 + wn * 16 * NB + ln), b = (n0 + wn * 16 * NB) * (int)sizeof(T) + 4 * ln;
 #pragma unroll
-    for (int q = 0; q < (16 * MB + 63) / 64; ++q) load_lds_4(ds, 4 * ln + 256 * q, to + 256 * q);
+    for (int q = 0; q < (16 * MB + 63) / 64; ++q) load_lds_4(sa_d, m + 256 * q, to + 256 * q);
 #pragma unroll
-    for (int q = 0; q < (16 * NB + 63) / 64; ++q) load_lds_4(dw, 4 * ln + 256 * q, to + 512 + 256 * q);
+    for (int q = 0; q < (16 * NB + 63) / 64; ++q) load_lds_4(sw_d, n + 256 * q, to + 512 + 256 * q);
 #pragma unroll
-    for (int q = 0; q < (16 * NB * (int)sizeof(T) + 255) / 256; ++q) load_lds_4(db, 4 * ln + 256 * q, to + 1024 + 256 * q);
+    for (int q = 0; q < (16 * NB * (int)sizeof(T) + 255) / 256; ++q) load_lds_4(bias_d, b + 256 * q, to + 1024 + 256 * q);
   };
   static_assert(LY >= 4, "the scales fit");
   // acc[2 k + h][j][e] = sum of row m, channel n of the tile, m = 16 MB wm + 16 j + fr, n = 16 NB wn + 32 k + 8 fh + 4 h + e
@@ -205,20 +236,22 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
 
   // One half: the MFMAs on f, among them the reads of the next half's fragments
   // into g (from ra and rw on) and the loads of X or Y into the slot at lds,
-  // fenced so that the compiler keeps this order.  A wave issues an instruction
+  // fenced so that the compiler keeps this order; `last` finds the next half's
+  // places among the last MFMAs.  A wave issues an instruction
   // every 4 cycles and an MFMA takes 16, so at most three others go between two
   // MFMAs.  The reads are in the order of their use, w0, a0 .., w1 ..; before
   // the barrier (X: false) they end early, so that they have landed there.
   constexpr int NM = MB * NB, NR = MB + NB;
-  auto half = [&](const Frags& f, Frags& g, int ra, int rw, uint32_t lds, auto loads_x, auto first) __attribute__((always_inline)) {
+  struct Places { int ra, rw; uint32_t lds; };   // bytes in LDS: the reads of A's and W's fragments, the loads
+  auto half = [&](const Frags& f, Frags& g, const Places& at, auto loads_x, auto first, auto&& last) __attribute__((always_inline)) {
     constexpr bool kX = decltype(loads_x)::value, kA = kX == XA;   // kA: the loads are A's
     constexpr int kReadStep = NM >= 64 ? (kX ? 4 : 3) : NM >= 48 && kX ? 3 : 2, kLoads = kX ? LX : LY;
     static_assert((NM - 1) / kReadStep + 1 >= NR && 4 * kLoads <= NM, "all reads and loads are issued");
     int vo[8];
-    auto prepare = [&](auto at) __attribute__((always_inline)) {
-      constexpr int u = decltype(at)::value;
+    auto prepare = [&](auto index) __attribute__((always_inline)) {
+      constexpr int u = decltype(index)::value;
       vo[u] = kA ? a_at[u & 1] + u * a_pc : w_at[u & 3] + u * w_pc;
-      load_lds_to<u * 1024>(lds, vo[u]);
+      load_lds_to<u * 1024>(at.lds, vo[u]);
     };
 #pragma unroll
     for (int m = 0; m < NM; ++m) {
@@ -227,9 +260,9 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
       else mfma16(acc[i][j], f.w[i], f.a[j]);
       const int r = m / kReadStep;
       if (m % kReadStep == 0 && r < NR) {
-        if (r == 0) g.w[0] = *reinterpret_cast<const i32x4*>(smem + rw);
-        else if (r <= MB) g.a[r - 1] = *reinterpret_cast<const i32x4*>(smem + ra + (r - 1) * 16 * kRowBytes);
-        else g.w[r - MB] = *reinterpret_cast<const i32x4*>(smem + rw + w_block(r - MB));
+        if (r == 0) g.w[0] = *reinterpret_cast<const i32x4*>(smem + at.rw);
+        else if (r <= MB) g.a[r - 1] = *reinterpret_cast<const i32x4*>(smem + at.ra + (r - 1) * 16 * kRowBytes);
+        else g.w[r - MB] = *reinterpret_cast<const i32x4*>(smem + at.rw + w_block(r - MB));
       }
       const int l = m / 4;
       if (m % 4 == 1 && l < kLoads) {
@@ -245,12 +278,15 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
         }
       }
       if (m % 4 == 3 && l < kLoads) load_lds_16(kA ? ad : wd, vo[l], l_off);
+      if (m == NM - 6) last(std::integral_constant<int, 0>{});
+      if (m == NM - 4) last(std::integral_constant<int, 1>{});
+      if (m == NM - 2) last(std::integral_constant<int, 2>{});
       __builtin_amdgcn_sched_barrier(0);
     }
   };
 
   // the first tile's steps 0 .. R - 1, then the fragments of step 0's first half
-  set_tile(0);
+  set_tile();
   set_step();
 #pragma unroll
   for (int s = 0; s < RX; ++s) {
@@ -266,40 +302,72 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
   for (int i = 0; i < NB; ++i) f0.w[i] = *reinterpret_cast<const i32x4*>(smem + fo_w[0] + w_block(i));
 #pragma unroll
   for (int j = 0; j < MB; ++j) f0.a[j] = *reinterpret_cast<const i32x4*>(smem + fo_a[0] + j * 16 * kRowBytes);
-  // slots of the current step, counted over all tiles, as bytes into the rings; tile coordinates as the cursor found them
-  int px = 0, py = 0;
-  auto next_x = [](int p) { return p == (RX - 1) * SX ? 0 : p + SX; };
-  auto next_y = [](int p) { return p == (RY - 1) * SY ? 0 : p + SY; };
-  auto last_y = [](int p) { return p == 0 ? (RY - 1) * SY : p - SY; };
-  constexpr int kStores = MB * NB / 2;                       // of a wave's epilogue
+  // slots of the current step, counted over all tiles, as bytes into the rings,
+  // and of the next; tile coordinates as the cursor found them.  A step's first
+  // half loads Y(s + R) into the slot of s - 1, its second X(s + R) into that of s.
+  int px = 0, py = 0, px1 = RX > 1 ? SX : 0, py1 = SY;
+  Places p1{fo_a[1], fo_w[1], lds_y + (RY - 1) * SY}, p2{};
+  auto to_second = [&](auto part) __attribute__((always_inline)) {
+    constexpr int k = decltype(part)::value;
+    if (k == 0) p2.lds = lds_x + px;
+    if (k == 1) p2.ra = fo_a[0] + (XA ? px1 : py1);
+    if (k == 2) p2.rw = fo_w[0] + (XA ? py1 : px1);
+    if (k == 0) asm volatile("" : "+s"(p2.lds));
+    if (k == 1) asm volatile("" : "+v"(p2.ra));
+    if (k == 2) asm volatile("" : "+v"(p2.rw));
+  };
+  auto to_first = [&](auto part) __attribute__((always_inline)) {
+    constexpr int k = decltype(part)::value;
+    if (k == 0) {
+      p1.lds = lds_y + py;
+      px = px1;
+      py = py1;
+      p1.ra = fo_a[1] + (XA ? px : py);
+    }
+    if (k == 1) {
+      p1.rw = fo_w[1] + (XA ? py : px);
+      px1 = px == (RX - 1) * SX ? 0 : px + SX;
+    }
+    if (k == 2) py1 = py == (RY - 1) * SY ? 0 : py + SY;
+    if (k == 0) asm volatile("" : "+s"(p1.lds));
+    if (k == 0) asm volatile("" : "+v"(p1.ra));
+    if (k == 1) asm volatile("" : "+v"(p1.rw));
+    if (k == 1) asm volatile("" : "+s"(px1));
+    if (k == 2) asm volatile("" : "+s"(py1));
+  };
+  constexpr int kStores = MB * NB / 2;                       // of a wave's epilogue, at least
   constexpr int kPending = (RX - 2) * LX + (RX - 1) * LY;    // loads that may be in flight at a step's barrier
   static_assert(kPending + kStores <= 63, "the counter's range");
   for (int it = 0; it < seq.count; ++it) {
     int tm = l_m, tn = l_n;   // the load cursor is in this tile, or, with few steps a tile, further on
     if (KT <= RX) seq.coords(it, tm, tn);
     const int m0 = tm * BM, n0 = tn * BN;
-    // A step's first half loads Y(s + R) into the slot of s - 1.  Then X(s + 1)
-    // and Y(s + 1) have to have landed; R - 2 steps of X and R - 1 of Y may still
-    // be in flight and, in a tile's first step, the stores of the tile before.
-    half(f0, f1, fo_a[1] + (XA ? px : py), fo_w[1] + (XA ? py : px), lds_y + last_y(py), std::false_type{}, std::true_type{});
+    half(f0, f1, p1, std::false_type{}, std::true_type{}, to_second);
+    // X(s + 1) and Y(s + 1) have to have landed; R - 2 steps of X and R - 1 of Y
+    // may still be in flight and, in a tile's first step, the stores of the tile before
     if (it == 0) wait_vmcnt<kPending>();
     else wait_vmcnt<kPending + kStores>();
     __syncthreads();
     __builtin_amdgcn_sched_barrier(0);
-    for (int s = 0;;) {
-      const int px1 = next_x(px), py1 = next_y(py);
-      if (s == KT - 1) load_scales(m0, n0, py);
-      // the second half loads X(s + R) into the slot of s
-      half(f1, f0, fo_a[0] + (XA ? px1 : py1), fo_w[0] + (XA ? py1 : px1), lds_x + px, std::true_type{}, std::false_type{});
+    auto step = [&]() __attribute__((always_inline)) {   // from the middle of a step to that of the next
+      half(f1, f0, p2, std::true_type{}, std::false_type{}, to_first);
       advance();
-      if (++s == KT) break;
-      px = px1;
-      py = py1;
-      half(f0, f1, fo_a[1] + (XA ? px : py), fo_w[1] + (XA ? py : px), lds_y + last_y(py), std::false_type{}, std::false_type{});
+      half(f0, f1, p1, std::false_type{}, std::false_type{}, to_second);
       wait_vmcnt<kPending>();
       __syncthreads();
       __builtin_amdgcn_sched_barrier(0);
+    };
+    int s = 1;
+    for (; s + 2 < KT; s += 3) {   // a taken branch stops the matrix cores for some 60 cycles
+      step();
+      step();
+      step();
     }
+    for (; s < KT; ++s) step();
+    const int scales = scales_at(py);   // in the last step's Y slot
+    load_scales(m0, n0, scales);
+    half(f1, f0, p2, std::true_type{}, std::false_type{}, to_first);
+    advance();
     // wait states from the last MFMA to a vector read of its result (the
     // compiler itself would put at most 12), and the scales, which only the last
     // step's X loads follow
@@ -321,7 +389,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
     int el = lane;
     asm volatile("" : "+v"(el));
     const int er = el & 15, eh = el >> 4;
-    const char* const sc = smem + scales_at(py);
+    const char* const sc = smem + scales;
     float wscale[NP][8], bias[NP][8];
     float row_scale[2];   // of this row block and the next
     row_scale[0] = *reinterpret_cast<const float*>(sc + 4 * er);
@@ -338,24 +406,27 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
     int out_at[NP], res_at[NP];   // lane offsets inside 16 rows
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-      const bool in = nw + 8 * eh + 32 * k < N;
-      out_at[k] = in ? (er * (int)ep.ldo + 8 * eh) * ES : (int)kNowhere;
-      res_at[k] = kRes && in ? (er * (int)ep.ldr + 8 * eh) * ES : (int)kNowhere;
+      const int n = 8 * eh + 32 * k;
+      out_at[k] = nw + n < N ? (er * (int)ep.ldo + n) * ES : (int)kNowhere;
+      res_at[k] = kRes && nw + n < N ? (er * (int)ep.ldr + n) * ES : (int)kNowhere;
+      asm volatile("" : "+v"(out_at[k]), "+v"(res_at[k]));   // formed once
     }
-    auto rows_of = [&](const T* p, int64_t ld, int j) {   // the wave's rows 16 j .. 16 j + 15 from its first channel on
-      const int m = mw + 16 * j;
-      return __builtin_amdgcn_make_buffer_rsrc((void*)(p + (int64_t)m * ld + nw), 0, m < M ? min(16, M - m) * (int)ld * ES : 0,
+    // the wave's rows 16 j .. 16 j + 15 from its first channel on
+    const char* const out0 = (const char*)(ep.out + (int64_t)mw * ep.ldo + nw);
+    const char* const res0 = kRes ? (const char*)(ep.res + (int64_t)mw * ep.ldr + nw) : nullptr;
+    auto rows_of = [&](const char* p, int64_t ld, int j) {
+      return __builtin_amdgcn_make_buffer_rsrc((void*)(p + j * (16 * ES * ld)), 0, max(0, min(16, M - mw - 16 * j)) * (int)ld * ES,
                                                0x00020000);
     };
     f32x4 rv[1 + kAhead][NP][ES / 2];
     auto load_res = [&](int j) __attribute__((always_inline)) {
       if constexpr (kRes) {
-        const auto d = rows_of(ep.res, ep.ldr, j);
+        const auto d = rows_of(res0, ep.ldr, j);
 #pragma unroll
         for (int k = 0; k < NP; ++k)
 #pragma unroll
           for (int q = 0; q < ES / 2; ++q)
-            rv[j & kAhead][k][q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(d, res_at[k] + 32 * ES * k + 16 * q, 0, 0));
+            rv[j & kAhead][k][q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(d, res_at[k] + 16 * q, 0, 0));
       }
     };
     if (kAhead) load_res(0);
@@ -379,7 +450,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
       if (j + 1 < MB) row_scale[(j + 1) & 1] = *reinterpret_cast<const float*>(sc + 4 * (16 * (j + 1) + er));
       if (j + kAhead < MB) load_res(j + kAhead);
       if (EPI == DIT_EPI_GATED_RESIDUAL && !g_one) load_gate(find_req(ep.req.cu, ep.req.n_req, min(mw + 16 * j + er, M - 1)));
-      const auto d = rows_of(ep.out, ep.ldo, j);
+      const auto d = rows_of(out0, ep.ldo, j);
 #pragma unroll
       for (int k = 0; k < NP; ++k) {
         __builtin_amdgcn_sched_barrier(0);   // more of them in flight cost spilled registers
@@ -400,19 +471,17 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
           u32x4 o;
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{z[2 * e], z[2 * e + 1]}, bf16x2));
-          __builtin_amdgcn_raw_buffer_store_b128(o, d, out_at[k] + 64 * k, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(o, d, out_at[k], 0, 0);
         } else {
 #pragma unroll
           for (int q = 0; q < 2; ++q)
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{z[4 * q], z[4 * q + 1], z[4 * q + 2], z[4 * q + 3]}), d,
-                                                   out_at[k] + 128 * k + 16 * q, 0, 0);
+                                                   out_at[k] + 16 * q, 0, 0);
         }
       }
     }
     // the scales are read before the next step's loads overwrite them, and no store moves behind those loads
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    px = next_x(px);
-    py = next_y(py);
   }
   wait_vmcnt<0>();   // no load may land in LDS after the workgroup has ended
 }

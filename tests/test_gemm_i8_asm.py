@@ -47,15 +47,18 @@ def test_accumulators_keep_their_distance(kernels):
 
 
 def test_k_loop_has_no_copies_and_no_full_waits(kernels):
-    """The halves of a step (and a tile's first half): no copies of accumulators, no spills, one wait for loads."""
+    """The halves of the steps: no copies of accumulators, no spills in the kernel, waits that leave loads in flight."""
     for name, body in kernels.items():
         assert not [l for l in body if "scratch_" in l], name
         halves = [b for b in _blocks(body) if any("v_mfma" in l for _, l, _ in b["ins"])]
-        assert len(halves) == 3, name
+        assert len(halves) >= 4, name
         ins = [l for b in halves for _, l, _ in b["ins"]]
-        assert not [l for l in ins if l.startswith(("v_accvgpr", "v_readlane", "v_writelane"))], name
+        assert not [l for l in ins if l.startswith(("v_accvgpr", "v_writelane"))], name
+        steady = [b for b in halves if not any(l.startswith("buffer_load_dword ") for _, l, _ in b["ins"])]
+        assert len(steady) == len(halves) - 1, name     # a tile's last half also loads the scales
+        assert not [l for b in steady for _, l, _ in b["ins"] if l.startswith("v_readlane")], name
         waits = [int(m.group(1)) for l in ins for m in re.finditer(r"vmcnt\((\d+)\)", l)]
-        assert len(waits) == 1 and waits[0] >= 6, f"{name}: vmcnt waits {waits}"
+        assert waits and min(waits) >= 6, f"{name}: vmcnt waits {waits}"
 
 
 def test_the_lds_address_of_a_load_is_the_one_set_for_it(kernels):

@@ -173,6 +173,41 @@ def test_waits_are_those_of_the_kernel():
     assert "wait_vmcnt<LX>();" in SRC
 
 
+@pytest.mark.parametrize("tiles_m,tiles_n,group_m,nb", [
+    (1, 1, 8, 8), (3, 7, 8, 256), (296, 60, 3, 256), (41, 54, 4, 256), (17, 3, 8, 256), (160, 1, 4, 256), (1, 999, 8, 248),
+    (9, 131072, 8, 256), (2048, 4, 3, 256), (5, 40, 8, 104)])
+def test_a_walk_over_the_tiles_is_tile_seq_s(tiles_m, tiles_n, group_m, nb):
+    """The walk without divisions, against the sequence's own coordinates: all tiles once, in the same order."""
+    tiles, width, total = tiles_m * tiles_n, group_m * tiles_n, 0
+    per_xcd = -(-tiles // 8)
+    for b in range(nb):
+        lo = b % 8 * per_xcd
+        first, stride, hi = lo + b // 8, nb // 8, min(tiles, lo + per_xcd)
+        count = -(-(hi - first) // stride) if first < hi else 0
+        total += count
+        if not count:
+            continue
+        t = first + stride * np.arange(count)
+        group = t // width
+        gsize = np.minimum(tiles_m - group * group_m, group_m)
+        r = t - group * width
+        want_m, want_n = group * group_m + r % gsize, r // gsize
+        assert want_m.max() < tiles_m and want_n.max() < tiles_n
+        # the walk
+        def regroup(m):
+            g = min(tiles_m - m, group_m)
+            return m, g, (0xFFFFFFFF // g + 1 if g > 1 else 0)
+        r, (first_m, g, inv) = first % width, regroup(first // width * group_m)
+        for i in range(count if count < 3000 else 300):
+            while r >= g * tiles_n:
+                r -= g * tiles_n
+                first_m, g, inv = regroup(first_m + g)
+            tn = r * inv >> 32 if g > 1 else r
+            assert (first_m + r - tn * g, tn) == (want_m[i], want_n[i])
+            r += stride
+    assert total == tiles
+
+
 FEW = 8
 
 

@@ -112,8 +112,8 @@ def linear(L, a=X, lda=64, sa=SC, w=W, ldw=64, sw=WS, bias=G, out=O, ldo=64, M=4
     (linear, dict(K=56), NOT, b"K % 16"),
     (linear, dict(N=60, ldo=64), NOT, b"N % 8"),
     (linear, dict(K=131072, lda=131072, ldw=131072), NOT, b"K <="),
-    (linear, dict(M=0x7FFFFF01), NOT, b"too many tiles"),
-    (linear, dict(M=1 << 30, N=1 << 20, ldo=1 << 20), NOT, b"too many tiles"),
+    (linear, dict(M=(1 << 28) + 1), NOT, b"too many tiles"),
+    (linear, dict(M=1 << 28, N=1 << 20, ldo=1 << 20), NOT, b"too many tiles"),
     (linear, dict(epi=4), BAD, b"epilogue"),
     (linear, dict(lda=48), BAD, b"lda"),
     (linear, dict(ldw=72), BAD, b"lda"),
