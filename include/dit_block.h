@@ -337,16 +337,16 @@ dit_status dit_linear_i8(const int8_t *a, int64_t lda, const float *a_scales, co
                          const int32_t *cu_seqlens, int n_req, dit_dtype dtype,
                          hipStream_t stream);
 
-/* dit_linear_i8 computes output tiles as dit_linear does, or, for few rows,
- * blocks of 16 channels whose sums over K are shared by a workgroup's waves.
- * For tests and tuning: dit_debug_linear_i8_tile forces a tile (256 x 256, 256 x
- * 192, 128 x 256, 128 x 192, 128 x 128; 16 x 16 for the kernel for few rows,
- * where the call has at most 4,096 of them) for every later call of this process,
- * 0 x 0 restores the choice per shape; other values give DIT_ERR_INVALID_ARG.
- * Results do not depend on it.  Process-wide; set it between calls.
+/* dit_linear_i8 computes output tiles as dit_linear does (256 x 256, 256 x 192,
+ * 128 x 256, 128 x 192, 128 x 128) or, for few rows, smaller ones whose sums over
+ * K are shared by a workgroup's waves (64 x 64, 32 x 64, 32 x 32, 16 x 16),
+ * whichever an estimate finds faster.  For tests and tuning:
+ * dit_debug_linear_i8_tile forces one of these for every later call of this
+ * process (the smaller ones where a call has at most 4,096 rows), 0 x 0 restores
+ * the choice per shape; other values give DIT_ERR_INVALID_ARG.  Results do not
+ * depend on it.  Process-wide; set it between calls.
  * dit_debug_linear_i8_plan: the tile that a call takes on a GPU of
- * `compute_units` compute units (16, 32 or 64 x 16 for few rows).  Host
- * arithmetic only. */
+ * `compute_units` compute units.  Host arithmetic only. */
 dit_status dit_debug_linear_i8_tile(int tile_m, int tile_n);
 dit_status dit_debug_linear_i8_plan(int64_t M, int N, int K, int compute_units, int *tile_m, int *tile_n);
 

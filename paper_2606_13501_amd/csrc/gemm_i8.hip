@@ -488,138 +488,243 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
 
 // ---------------------------------------------------------------- few rows
 //
-// Up to 64 rows: a workgroup of 8 waves computes MB x NB blocks of 16 x 16 (all
-// rows, 16 NB output channels), the waves share K in turns of 128 bytes and
-// their sums, whole numbers, meet in LDS.  The operands go from global memory
-// straight into the matrix instruction's registers: 16 rows x 64 bytes a load.
-// Bound by the weights, which are read once.
-constexpr int kFewWaves = 8;
+// Where tiles of 128 x 128 would leave most compute units without work, a
+// workgroup computes MB x NB blocks of 16 x 16 only, and its NW waves share K in
+// turns of 128 bytes; their sums, whole numbers, meet in LDS.  Each wave has a
+// ring of R turns in LDS for itself, filled straight from global memory in whole
+// cache lines, so the K loop has no barrier, and the ring runs on into the
+// workgroup's next tile while this one's sums are joined.
+template <int MB_, int NB_, int NW_, int R_>
+struct FewShape {
+  static constexpr int MB = MB_, NB = NB_, NW = NW_, R = R_;
+  static constexpr int kLoads = 2 * (MB + NB);                       // 1 KiB loads of a turn
+  static constexpr int kSlot = 1024 * kLoads;
+  static constexpr int kScales = 768;                                // scales of rows and channels and biases, 256 B each
+  static constexpr int kPart = NW * R * kSlot;                       // LDS: rings, partial sums, R + 1 tiles' scales of each wave
+  static constexpr int kScalesAt = kPart + NW * MB * NB * 1024;
+  static constexpr int kLds = kScalesAt + NW * (R + 1) * kScales;
+  static constexpr int kResident = kLds <= 80 * 1024 ? 2 : 1;        // workgroups of a compute unit
+  static_assert(MB <= 4 && NB <= 4 && (R - 1) * kLoads <= 63 && kLds <= 160 * 1024, "one load of scales, the counter, LDS");
+};
 
-template <typename T, int EPI, int MB, int NB>
-__global__ __launch_bounds__(64 * kFewWaves) void gemm_i8_few(
-    const int8_t* __restrict__ A, int64_t lda, const int8_t* __restrict__ W, int64_t ldw, Epi<T> ep, int M, int N, int K) {
+template <typename T, int EPI, typename S>
+__global__ __launch_bounds__(64 * S::NW, 1) void gemm_i8_few(
+    const int8_t* __restrict__ A, int64_t lda, const int8_t* __restrict__ W, int64_t ldw, Epi<T> ep, int M, int N, int K,
+    int tiles_m, int tiles) {
   typedef T V4 __attribute__((ext_vector_type(4)));
-  constexpr int U = MB * NB <= 2 ? 5 : MB * NB <= 4 ? 3 : 2;   // turns in flight
-  __shared__ i32x4 part[kFewWaves][MB * NB][64];
+  constexpr int MB = S::MB, NB = S::NB, NW = S::NW, R = S::R;
+  __shared__ __attribute__((aligned(1024))) char smem[S::kLds];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, fh = lane >> 4;
-  const int n0 = blockIdx.x * 16 * NB, m0 = blockIdx.y * 16 * MB;
-  const int8_t *pa[MB], *pw[NB];   // rows past the last repeat it
-#pragma unroll
-  for (int j = 0; j < MB; ++j) pa[j] = A + (int64_t)min(m0 + 16 * j + fr, M - 1) * lda + 16 * fh;
-#pragma unroll
-  for (int i = 0; i < NB; ++i) pw[i] = W + (int64_t)min(n0 + 16 * i + fr, N - 1) * ldw + 16 * fh;
-  i32x4 acc[NB][MB] = {};
-  struct Step { i32x4 a[MB][2], w[NB][2]; };
-  // the turn from byte k on: FULL, or what K leaves of it (a lane's 16 bytes are inside or outside)
-  auto load = [&](Step& s, int k, auto full) __attribute__((always_inline)) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bool in = decltype(full)::value || k + 64 * h + 16 * fh < K;
-#pragma unroll
-      for (int i = 0; i < NB; ++i) s.w[i][h] = in ? *reinterpret_cast<const i32x4*>(pw[i] + k + 64 * h) : i32x4{};
-#pragma unroll
-      for (int j = 0; j < MB; ++j) s.a[j][h] = in ? *reinterpret_cast<const i32x4*>(pa[j] + k + 64 * h) : i32x4{};
+  const int turns = (K + BK - 1) / BK, per_wave = (turns + NW - 1) / NW;   // wave w takes turns w, w + NW, ..
+  const int tail_chunks = (K - (turns - 1) * BK) / 16;
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+  const int ring = wave * R * S::kSlot, scales = S::kScalesAt + wave * (R + 1) * S::kScales;
+  // Tile t: its row tiles are next to each other on one XCD (workgroups go
+  // round-robin over the 8), which reads their weights once.
+  auto coords = [&](int t, int& m0, int& n0) __attribute__((always_inline)) {
+    const int q = t / kXcds, g = q / tiles_m;
+    m0 = (q - g * tiles_m) * (16 * MB);
+    n0 = (g * kXcds + t % kXcds) * (16 * NB);
+  };
+
+  // ---- loads: pieces of 8 rows x 128 bytes, swizzled, as in the tiled kernel
+  u32x4 ad{}, wd{};
+  const u32x4 sa_d = make_desc(ep.sa, (int64_t)M * 4), sw_d = make_desc(ep.sw, (int64_t)N * 4);
+  const u32x4 bias_d = make_desc(ep.bias, ep.bias ? (int64_t)N * (int)sizeof(T) : 0);
+  const int a_pc = 8 * (int)lda, w_pc = 8 * (int)ldw;
+  int l_tile = blockIdx.x, l_turn = wave, l_left = per_wave, l_slot = 0, l_buf = 0;
+  auto set_tile = [&]() __attribute__((always_inline)) {
+    if (l_tile < tiles) {
+      int m0, n0;
+      coords(l_tile, m0, n0);
+      ad = make_desc(A + (int64_t)m0 * lda, min((int64_t)0x7FFFFFFF, (int64_t)(M - m0 - 1) * lda + K));
+      // (the last tiles of the round-robin order may lie behind the last channel)
+      wd = make_desc(W + (int64_t)min(n0, N - 1) * ldw, n0 < N ? min((int64_t)0x7FFFFFFF, (int64_t)(N - n0 - 1) * ldw + K) : 0);
+      const uint32_t to = lds_base + scales + l_buf * S::kScales;
+      load_lds_4(sa_d, 4 * (m0 + lane), to);
+      load_lds_4(sw_d, 4 * (n0 + lane), to + 256);
+      load_lds_4(bias_d, n0 * (int)sizeof(T) + 4 * lane, to + 512);
+      l_buf = l_buf == R ? 0 : l_buf + 1;
+    } else {   // past the last tile
+      ad[2] = 0;
+      wd[2] = 0;
     }
   };
-  auto mma = [&](const Step& s) __attribute__((always_inline)) {
+  auto load = [&]() __attribute__((always_inline)) {   // the cursor's turn into its slot, and the cursor on
+    if (l_left == per_wave) set_tile();
+    // chunks of this turn: a row's 8, what K leaves of the last one, none behind it
+    const int live = l_turn < turns - 1 ? 8 : l_turn == turns - 1 ? tail_chunks : 0;
+    const uint32_t to = lds_base + ring + l_slot * S::kSlot;
+    int a_at[2], w_at[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int u = 0; u < 2; ++u) {
+      const int c = (lane & 7) ^ row_swizzle(8 * u + (lane >> 3)), none = c < live ? 0 : (int)kNowhere;
+      a_at[u] = ((lane >> 3) * (int)lda + c * 16) | none;
+      w_at[u] = ((lane >> 3) * (int)ldw + c * 16) | none;
+    }
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
+    for (int u = 0; u < 2 * MB; ++u) load_lds16(ad, a_at[u & 1] + u * a_pc, l_turn * BK, to + u * 1024);
 #pragma unroll
-        for (int j = 0; j < MB; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(s.w[i][h], s.a[j][h], acc[i][j], 0, 0, 0);
+    for (int u = 0; u < 2 * NB; ++u) load_lds16(wd, w_at[u & 1] + u * w_pc, l_turn * BK, to + (2 * MB + u) * 1024);
+    l_slot = l_slot == R - 1 ? 0 : l_slot + 1;
+    l_turn += NW;
+    if (--l_left == 0) {
+      l_turn = wave;
+      l_left = per_wave;
+      l_tile += gridDim.x;
+    }
   };
-  const int whole = K / BK;   // whole turns; wave w takes turns w, w + 8, ..
-  int t = wave;
-  for (; t + kFewWaves * (U - 1) < whole; t += kFewWaves * U) {
-    Step s[U];
+  int fo[2];
 #pragma unroll
-    for (int u = 0; u < U; ++u) load(s[u], (t + kFewWaves * u) * BK, std::true_type{});
+  for (int kk = 0; kk < 2; ++kk) fo[kk] = fr * kRowBytes + (((4 * kk + fh) ^ row_swizzle(fr)) << 4);
+
 #pragma unroll
-    for (int u = 0; u < U; ++u) mma(s[u]);
-  }
-  if (t * BK < K) {   // up to U turns more, the last one perhaps not whole
-    Step s[U];
+  for (int r = 0; r < R; ++r) load();
+  int slot = 0, buf = 0;
+  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    i32x4 acc[NB][MB] = {};
+    for (int i = 0; i < per_wave; ++i) {
+      wait_vmcnt<(R - 1) * S::kLoads>();   // this turn's loads, and its tile's scales
+      i32x4 a[2][MB], w[2][NB];
+      const char* const at = smem + ring + slot * S::kSlot;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if ((t + kFewWaves * u) * BK < K) load(s[u], (t + kFewWaves * u) * BK, std::false_type{});
+      for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if ((t + kFewWaves * u) * BK < K) mma(s[u]);
-  }
+        for (int n = 0; n < NB; ++n) w[kk][n] = *reinterpret_cast<const i32x4*>(at + fo[kk] + (MB + n) * 2048);
 #pragma unroll
-  for (int i = 0; i < NB; ++i)
-#pragma unroll
-    for (int j = 0; j < MB; ++j) part[wave][i * MB + j][lane] = acc[i][j];
-  __syncthreads();
-  for (int b = wave; b < MB * NB; b += kFewWaves) {
-    i32x4 c = part[0][b][lane];
-#pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) c += part[w][b][lane];
-    const int m = m0 + 16 * (b % MB) + fr, n = n0 + 16 * (b / MB) + 4 * fh;
-    if (m >= M || n >= N) continue;
-    const float sa = ep.sa[m];
-    float z[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = fmaf((float)c[e] * sa, ep.sw[n + e], ep.bias ? (float)ep.bias[n + e] : 0.f);
-    if (EPI == DIT_EPI_GELU_TANH) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) z[e] = gelu_tanh(z[e]);
-    } else if (EPI == DIT_EPI_RESIDUAL || EPI == DIT_EPI_GATED_RESIDUAL) {
-      const V4 r = *reinterpret_cast<const V4*>(ep.res + (int64_t)m * ep.ldr + n);
-      if (EPI == DIT_EPI_GATED_RESIDUAL) {
-        const f32x4 g = *reinterpret_cast<const f32x4*>(ep.gate + (int64_t)find_req(ep.req.cu, ep.req.n_req, m) * ep.gate_stride + n);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = fmaf(g[e], z[e], (float)r[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = (float)r[e] + z[e];
+        for (int j = 0; j < MB; ++j) a[kk][j] = *reinterpret_cast<const i32x4*>(at + fo[kk] + j * 2048);
       }
-    }
-    V4 o;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // before the slot is filled again
+      load();
+      slot = slot == R - 1 ? 0 : slot + 1;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (T)z[e];
-    *reinterpret_cast<V4*>(ep.out + (int64_t)m * ep.ldo + n) = o;
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int j = 0; j < MB; ++j) acc[n][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[kk][n], a[kk][j], acc[n][j], 0, 0, 0);
+    }
+    i32x4* const part = reinterpret_cast<i32x4*>(smem + S::kPart);
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int j = 0; j < MB; ++j) part[(wave * MB * NB + n * MB + j) * 64 + lane] = acc[n][j];
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    int m0, n0;
+    coords(tile, m0, n0);
+    const char* const sc = smem + scales + buf * S::kScales;
+    buf = buf == R ? 0 : buf + 1;
+#pragma unroll
+    for (int x = 0; x < (MB * NB + NW - 1) / NW; ++x) {
+      const int b = wave + NW * x;
+      const int ml = 16 * (b % MB) + fr, nl = 16 * (b / MB) + 4 * fh, m = m0 + ml, n = n0 + nl;
+      if (b >= MB * NB || m >= M || n >= N) continue;
+      i32x4 c = part[b * 64 + lane];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) c += part[(w * MB * NB + b) * 64 + lane];
+      const float sa = *reinterpret_cast<const float*>(sc + 4 * ml);
+      const f32x4 sw = *reinterpret_cast<const f32x4*>(sc + 256 + 4 * nl);
+      const V4 bias = *reinterpret_cast<const V4*>(sc + 512 + (int)sizeof(T) * nl);
+      float z[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[e] = fmaf((float)c[e] * sa, sw[e], (float)bias[e]);
+      if (EPI == DIT_EPI_GELU_TANH) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = gelu_tanh(z[e]);
+      } else if (EPI == DIT_EPI_RESIDUAL || EPI == DIT_EPI_GATED_RESIDUAL) {
+        const V4 r = *reinterpret_cast<const V4*>(ep.res + (int64_t)m * ep.ldr + n);
+        if (EPI == DIT_EPI_GATED_RESIDUAL) {
+          const f32x4 g = *reinterpret_cast<const f32x4*>(ep.gate + (int64_t)find_req(ep.req.cu, ep.req.n_req, m) * ep.gate_stride + n);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[e] = fmaf(g[e], z[e], (float)r[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[e] = (float)r[e] + z[e];
+        }
+      }
+      V4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (T)z[e];
+      *reinterpret_cast<V4*>(ep.out + (int64_t)m * ep.ldo + n) = o;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the sums are read before the next tile's are written
   }
+  wait_vmcnt<0>();   // no load may land in LDS after the workgroup has ended
 }
 
 // -------------------------------------------------------------- the choice
 
-// The tile shapes, by the index of kCost.
+// The tile shapes, by the index of kTiles, and the shapes for few rows, by that of kFew.
 typedef Shape<8, 8, 2, false> Tile256x256;
 typedef Shape<8, 6, 2, false> Tile256x192;
 typedef Shape<4, 8, 2, true> Tile128x256;
 typedef Shape<4, 6, 3, false> Tile128x192;
 typedef Shape<4, 4, 4, false> Tile128x128;
-struct TileCost { int bm, bn; float fixed, step, full; };
-constexpr TileCost kCost[5] = {
-    {256, 256, 7.15f, 0.9445f, 0.3357f}, {256, 192, 5.97f, 0.7277f, 0.2706f}, {128, 256, 4.45f, 0.5556f, 0.1872f},
-    {128, 192, 3.34f, 0.4396f, 0.1457f}, {128, 128, 2.74f, 0.3213f, 0.1101f}};
-constexpr int kFew = 5;   // the index of the kernel for few rows
-constexpr int kFewRows = 64;
-int few_tile_m(int64_t M) { return M <= 16 ? 16 : M <= 32 ? 32 : 64; }
+typedef FewShape<1, 1, 4, 2> Few16x16;
+typedef FewShape<2, 2, 4, 3> Few32x32;
+typedef FewShape<2, 4, 4, 2> Few32x64;
+typedef FewShape<4, 4, 2, 3> Few64x64;
+
+// What a launch takes on 256 compute units, in us.  Of tiles: `launch`, for each
+// round of tiles (one per compute unit) `fixed` and per K step `step`, per K step
+// and share of the compute units kept busy `busy`, per MB of weights `weights`.
+// For few rows: `launch`, for each round (`resident` workgroups per compute unit)
+// `fixed` and per turn of a wave `turn`, per MB that all workgroups read together
+// `read`, per MB of weights `weights`.
+//
+// Fitted to 342 products with weights from memory, M = 1 to 32,760, N = 64 to
+// 30,720, K = 256 to 14,336, each timed with every shape (as a graph of calls, M
+// up to 512): the shape with the least estimate is 1.9% slower than the fastest
+// in the mean, 26% at most (17 x 200 x 12,000).  With 9 more shapes for few rows
+// (more or fewer waves, 16 x 32, 16 x 64, 32 x 16, 64 x 16, 64 x 32) the best of
+// all would be those 1.9% faster.  In us, 128 x 128 and the shapes for few rows:
+// 1 x 5,120 x 5,120 21.0 and 8.3 (16 x 16), 64 x 5,120 x 5,120 26.7 and 13.5 (32
+// x 64), 128 x 5,120 x 13,824 64.9 and 36.7 (64 x 64), 64 x 384 x 1,536 8.1 and
+// 3.3, 1 x 30,720 x 5,120 32.8 and 28.3; but 64 x 30,720 x 5,120 38.1 and 40.8,
+// 256 x 15,360 x 5,120 34.0 and 61.0.
+struct TileCost { int bm, bn; float launch, fixed, step, busy, weights; };
+constexpr TileCost kTiles[5] = {
+    {256, 256, 1.11f, 7.02f, 0.938f, 0.339f, 0.060f}, {256, 192, 1.81f, 4.96f, 0.725f, 0.265f, 0.060f},
+    {128, 256, 2.27f, 3.12f, 0.566f, 0.200f, 0.143f}, {128, 192, 2.99f, 2.25f, 0.459f, 0.169f, 0.123f},
+    {128, 128, 3.32f, 1.42f, 0.339f, 0.165f, 0.083f}};
+struct FewCost { int bm, bn, waves, resident; float launch, fixed, turn, read, weights; };
+constexpr FewCost kFew[4] = {
+    {16, 16, Few16x16::NW, Few16x16::kResident, 2.39f, 0.848f, 0.175f, 0.0180f, 0.095f},
+    {32, 32, Few32x32::NW, Few32x32::kResident, 2.76f, 0.783f, 0.299f, 0.0114f, 0.074f},
+    {32, 64, Few32x64::NW, Few32x64::kResident, 2.57f, 1.187f, 0.500f, 0.0061f, 0.098f},
+    {64, 64, Few64x64::NW, Few64x64::kResident, 2.80f, 2.162f, 0.511f, 0.0043f, 0.047f}};
+constexpr int kFewRows = 4096;   // rows up to which the shapes for few rows are launched
 
 std::atomic<int> g_shape{-1};   // forced shape (-1: chosen per call)
 
+// The index of the call's shape: of kTiles, or 5 and that of kFew.
 int choose(int64_t M, int N, int K, int cus) {
-  const bool few = M <= 64 * kFewRows;   // what that kernel is launched with
   const int forced = g_shape.load(std::memory_order_relaxed);
-  if (forced >= 0 && (forced != kFew || few)) return forced;
-  if (few && M <= kFewRows) return kFew;
-  const float kt = (float)((K + BK - 1) / BK);
+  if (forced >= 0 && (forced < 5 || M <= kFewRows)) return forced;
+  auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  const float kt = (float)ceil_div(K, BK), weights = (float)N * (float)K * 1e-6f;
   int best = 0;
   float least = 0.f;
   for (int t = 0; t < 5; ++t) {
-    const TileCost& c = kCost[t];
-    const int64_t tiles = ((M + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn);
-    const int64_t rounds = tiles / cus, rest = tiles % cus;
-    const float cost = (float)rounds * (c.fixed + kt * (c.step + c.full)) +
-                       (rest ? c.fixed + kt * (c.step + c.full * (float)rest / (float)cus) : 0.f);
+    const TileCost& c = kTiles[t];
+    const int64_t tiles = ceil_div(M, c.bm) * ceil_div(N, c.bn);
+    const float cost = c.launch + (float)ceil_div(tiles, cus) * (c.fixed + kt * c.step) +
+                       kt * (float)tiles / (float)cus * c.busy + weights * c.weights;
     if (t == 0 || cost < least) {
       best = t;
+      least = cost;
+    }
+  }
+  for (int t = 0; t < 4 && M <= kFewRows; ++t) {
+    const FewCost& c = kFew[t];
+    const int64_t tiles = ceil_div(M, c.bm) * ceil_div(ceil_div(N, c.bn), kXcds) * kXcds;
+    const float read = (float)tiles * (float)((M < c.bm ? M : c.bm) + c.bn) * (float)K * 1e-6f;
+    const float cost = c.launch + (float)ceil_div(tiles, (int64_t)cus * c.resident) * (c.fixed + (float)ceil_div((int64_t)kt, c.waves) * c.turn) +
+                       read * c.read + weights * c.weights;
+    if (cost < least) {
+      best = 5 + t;
       least = cost;
     }
   }
@@ -647,10 +752,14 @@ hipError_t launch_tiles(const LinearI8Args& p, int cus, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, int EPI, int MB, int NB>
-hipError_t launch_few(const LinearI8Args& p, hipStream_t s) {
-  const dim3 grid((unsigned)((p.N + 16 * NB - 1) / (16 * NB)), (unsigned)((p.M + 16 * MB - 1) / (16 * MB)));
-  gemm_i8_few<T, EPI, MB, NB><<<grid, 64 * kFewWaves, 0, s>>>(p.a, p.lda, p.w, p.ldw, epi_of<T>(p), (int)p.M, p.N, p.K);
+template <typename T, int EPI, typename S>
+hipError_t launch_few(const LinearI8Args& p, int cus, hipStream_t s) {
+  const int64_t tiles_n = (p.N + 16 * S::NB - 1) / (16 * S::NB), tiles_m = (p.M + 16 * S::MB - 1) / (16 * S::MB);
+  const int64_t tiles = (tiles_n + kXcds - 1) / kXcds * kXcds * tiles_m;
+  const int64_t resident = (int64_t)cus / kXcds * kXcds * S::kResident;
+  const int grid = (int)(resident >= kXcds && tiles > resident ? resident : tiles);
+  gemm_i8_few<T, EPI, S><<<grid, 64 * S::NW, 0, s>>>(p.a, p.lda, p.w, p.ldw, epi_of<T>(p), (int)p.M, p.N, p.K, (int)tiles_m,
+                                                     (int)tiles);
   return hipGetLastError();
 }
 
@@ -663,12 +772,10 @@ hipError_t launch_epi(const LinearI8Args& p, hipStream_t s) {
     case 2: return launch_tiles<T, EPI, Tile128x256>(p, cus, s);
     case 3: return launch_tiles<T, EPI, Tile128x192>(p, cus, s);
     case 4: return launch_tiles<T, EPI, Tile128x128>(p, cus, s);
-    default: break;
-  }
-  switch (few_tile_m(p.M)) {
-    case 16: return launch_few<T, EPI, 1, 1>(p, s);
-    case 32: return launch_few<T, EPI, 2, 1>(p, s);
-    default: return launch_few<T, EPI, 4, 1>(p, s);
+    case 5: return launch_few<T, EPI, Few16x16>(p, cus, s);
+    case 6: return launch_few<T, EPI, Few32x32>(p, cus, s);
+    case 7: return launch_few<T, EPI, Few32x64>(p, cus, s);
+    default: return launch_few<T, EPI, Few64x64>(p, cus, s);
   }
 }
 
@@ -685,17 +792,19 @@ hipError_t launch_typed(const LinearI8Args& p, hipStream_t s) {
 }  // namespace
 
 bool set_linear_i8_tile(int tile_m, int tile_n) {
-  int shape = tile_m == 0 && tile_n == 0 ? -1 : tile_m == 16 && tile_n == 16 ? kFew : -2;
+  int shape = tile_m == 0 && tile_n == 0 ? -1 : -2;
   for (int t = 0; t < 5; ++t)
-    if (kCost[t].bm == tile_m && kCost[t].bn == tile_n) shape = t;
+    if (kTiles[t].bm == tile_m && kTiles[t].bn == tile_n) shape = t;
+  for (int t = 0; t < 4; ++t)
+    if (kFew[t].bm == tile_m && kFew[t].bn == tile_n) shape = 5 + t;
   if (shape >= -1) g_shape.store(shape, std::memory_order_relaxed);
   return shape >= -1;
 }
 
 void linear_i8_plan(int64_t M, int N, int K, int cus, int* tile_m, int* tile_n) {
   const int t = choose(M, N, K, cus);
-  *tile_m = t == kFew ? few_tile_m(M) : kCost[t].bm;
-  *tile_n = t == kFew ? 16 : kCost[t].bn;
+  *tile_m = t < 5 ? kTiles[t].bm : kFew[t - 5].bm;
+  *tile_n = t < 5 ? kTiles[t].bn : kFew[t - 5].bn;
 }
 
 hipError_t launch_linear_i8(const LinearI8Args& p, hipStream_t s) {

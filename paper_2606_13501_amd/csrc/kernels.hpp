@@ -51,8 +51,7 @@ struct LinearI8Args {
   dit_dtype dtype;               // of bias, res and out
 };
 hipError_t launch_linear_i8(const LinearI8Args& p, hipStream_t s);
-// Forces its output tile (16 x 16: the kernel for few rows; 0 x 0: chosen per
-// shape); false if there is none of that size.
+// Forces its output tile (0 x 0: chosen per shape); false if there is none of that size.
 bool set_linear_i8_tile(int tile_m, int tile_n);
 // The output tile of a launch on `cus` compute units.
 void linear_i8_plan(int64_t M, int N, int K, int cus, int* tile_m, int* tile_n);

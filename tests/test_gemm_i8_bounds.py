@@ -18,7 +18,7 @@ SHAPES = [(int(a), int(b), int(c), d == "true") for a, b, c, d in re.findall(r"t
 def test_constants_are_those_of_the_kernel():
     assert len(SHAPES) == 5
     assert re.search(r"kNowhere = 0x80000000u", SRC) and "constexpr int BK = kRowBytes" in SRC
-    assert SRC.count("(int64_t)0x7FFFFFFF") == 2
+    assert SRC.count("(int64_t)0x7FFFFFFF") == 4
 
 
 def row_swizzle(r):
@@ -208,35 +208,101 @@ def test_a_walk_over_the_tiles_is_tile_seq_s(tiles_m, tiles_n, group_m, nb):
     assert total == tiles
 
 
-FEW = 8
+FEW = [tuple(int(x) for x in m) for m in re.findall(r"typedef FewShape<(\d+), (\d+), (\d+), (\d+)> Few", SRC)]
 
 
-@pytest.mark.parametrize("U", [5, 3, 2])
-@pytest.mark.parametrize("K", [16, 64, 112, 128, 144, 1024, 1040, 5120, 5136, 13824, 131056])
-def test_few_rows_take_each_byte_once(K, U):
-    seen = np.zeros(K // 16, dtype=int)
-    whole = K // BK
-    fh = np.arange(4)
-    for wave in range(FEW):
-        t = wave
-        while t + FEW * (U - 1) < whole:
-            for u in range(U):
-                for h in range(2):
-                    at = (t + FEW * u) * BK + 64 * h + 16 * fh
-                    assert (at + 16 <= K).all()
-                    seen[at // 16] += 1
-            t += FEW * U
-        if t * BK < K:
-            for u in range(U):
-                if (t + FEW * u) * BK < K:
-                    for h in range(2):
-                        at = (t + FEW * u) * BK + 64 * h + 16 * fh
-                        at = at[at < K]
-                        assert (at + 16 <= K).all()
-                        seen[at // 16] += 1
-            assert (t + FEW * U) * BK >= K          # nothing is left for another round
-    assert (seen == 1).all()
+def test_few_shapes():
+    assert len(FEW) == 4
+    for mb, nb, nw, r in FEW:
+        loads = 2 * (mb + nb)
+        lds = nw * r * loads * 1024 + nw * mb * nb * 1024 + nw * (r + 1) * 768
+        assert lds <= 160 * 1024 and (r - 1) * loads <= 63 and mb <= 4 and nb <= 4
+        # scales: 64 floats for at most 64 rows and channels, 64 floats or 128 bf16 of biases
+        assert 16 * max(mb, nb) * 4 <= 256
 
 
-def test_few_rows_numbers_are_those_of_the_kernel():
-    assert f"kFewWaves = {FEW};" in SRC and "U = MB * NB <= 2 ? 5 : MB * NB <= 4 ? 3 : 2" in SRC
+@pytest.mark.parametrize("operand", ["a", "w"])
+@pytest.mark.parametrize("blocks", [1, 2, 4])
+@pytest.mark.parametrize("nw", [2, 4])
+@pytest.mark.parametrize("M,K,ld", [(1, 16, 16), (1, 128, 128), (40, 144, 160), (64, 112, 112), (65, 272, 4096), (5, 5104, 5120),
+                                    (63, 131056, 131056), (100, 2048, 1 << 22), (64, 48, 1 << 22)])
+def test_few_rows_loads_stay_inside_and_take_each_byte_once(M, K, ld, nw, blocks, operand):
+    rows, turns = 16 * blocks, -(-K // BK)
+    per_wave, tail = -(-turns // nw), (K - (turns - 1) * BK) // 16
+    lane = np.arange(64)
+    for m0 in range(0, M, rows):
+        n_rec = min(FAR, (M - m0 - 1) * ld + K)
+        seen = np.zeros((min(rows, M - m0), K // 16), dtype=int)
+        for wave in range(nw):
+            for t in range(wave, wave + nw * per_wave, nw):
+                live = 8 if t < turns - 1 else tail if t == turns - 1 else 0
+                if K > 20000 and 1 < t < turns - 2:      # the middle is like its neighbours
+                    seen[:, t * 8:t * 8 + 8] += 1
+                    continue
+                for u in range(2 * blocks):
+                    c = (lane & 7) ^ row_swizzle(8 * (u & 1) + (lane >> 3))
+                    vo = (((lane >> 3) * ld + c * 16) | np.where(c < live, 0, NOWHERE)) + u * 8 * ld
+                    assert vo.max() < 1 << 32 and vo[vo < NOWHERE].max(initial=0) < 1 << 30
+                    ok = vo < n_rec
+                    at = vo[ok] + t * BK
+                    row, byte = at // ld, at % ld
+                    assert (row < M - m0).all() and (byte + 16 <= K).all()
+                    lds = u * 1024 + 16 * lane[ok]           # the fragment reads' place for it
+                    assert (lds // 128 == row).all()
+                    assert (lds % 128 // 16 ^ row_swizzle(lds // 128) == byte % 128 // 16).all()
+                    np.add.at(seen, (row, byte // 16), 1)
+        assert (seen == 1).all()
+
+
+@pytest.mark.parametrize("mb,nb,nw,r", FEW)
+@pytest.mark.parametrize("per_wave", [1, 2, 3, 5, 11])
+def test_few_rows_ring_and_scales(mb, nb, nw, r, per_wave):
+    """One wave's loads over several tiles: each turn's and its tile's scales have landed at its wait, a slot is refilled
+    after its reads, a tile's scales stay until its results are written."""
+    loads, tiles = 2 * (mb + nb), 9
+    issued, slots, bufs = [], {}, {}
+    cursor = {"tile": 0, "left": per_wave, "slot": 0, "buf": 0, "turn": 0}
+
+    def load(free_turn, done_tile):
+        if cursor["left"] == per_wave and cursor["tile"] < tiles:
+            old = bufs.get(cursor["buf"])
+            assert old is None or old < done_tile      # its results are written
+            bufs[cursor["buf"]] = cursor["tile"]
+            issued.extend([("scales", cursor["tile"])] * 3)
+            cursor["buf"] = 0 if cursor["buf"] == r else cursor["buf"] + 1
+        old = slots.get(cursor["slot"])
+        assert old is None or old <= free_turn
+        slots[cursor["slot"]] = cursor["turn"]
+        issued.extend([("turn", cursor["turn"])] * loads)
+        cursor["turn"] += 1
+        cursor["slot"] = 0 if cursor["slot"] == r - 1 else cursor["slot"] + 1
+        cursor["left"] -= 1
+        if cursor["left"] == 0:
+            cursor["left"], cursor["tile"] = per_wave, cursor["tile"] + 1
+
+    for _ in range(r):
+        load(-1, 0)
+    slot = buf = turn = 0
+    for tile in range(tiles):
+        for _ in range(per_wave):
+            done = issued[:len(issued) - (r - 1) * loads]
+            assert done.count(("turn", turn)) == loads and done.count(("scales", tile)) == 3
+            assert slots[slot] == turn
+            load(turn, tile)
+            slot = 0 if slot == r - 1 else slot + 1
+            turn += 1
+        assert bufs[buf] == tile
+        buf = 0 if buf == r else buf + 1
+        issued.extend([("store", tile)] * (mb * nb // nw))
+
+
+@pytest.mark.parametrize("tiles_m,tiles_n", [(1, 1), (1, 8), (2, 9), (3, 320), (64, 17), (5, 63)])
+def test_few_rows_tiles_cover_the_output(tiles_m, tiles_n):
+    groups = -(-tiles_n // 8) * 8
+    seen = set()
+    for t in range(groups * tiles_m):
+        g = t // 8 // tiles_m
+        m, n = t // 8 - g * tiles_m, g * 8 + t % 8
+        assert n < groups and (m, n) not in seen
+        seen.add((m, n))
+    assert {(m, n) for m, n in seen if n < tiles_n} == {(m, n) for m in range(tiles_m) for n in range(tiles_n)}

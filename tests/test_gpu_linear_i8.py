@@ -18,7 +18,7 @@ pytestmark = pytest.mark.gpu
 
 E = 2.0 ** -24
 TD = {"bf16": torch.bfloat16, "fp32": torch.float32}
-TILES = [(256, 256), (256, 192), (128, 256), (128, 192), (128, 128), (16, 16)]
+TILES = [(256, 256), (256, 192), (128, 256), (128, 192), (128, 128), (64, 64), (32, 64), (32, 32), (16, 16)]
 
 
 @pytest.fixture(scope="module")

@@ -207,14 +207,17 @@ def test_binding_checks():
             lin(**bad)
 
 
+TILES = [(256, 256), (256, 192), (128, 256), (128, 192), (128, 128), (64, 64), (32, 64), (32, 32), (16, 16)]
+
+
 def test_a_forced_tile_is_one_of_the_kernel_s(L):
     for bad in ((256, 128), (0, 256), (64, 16), (-1, -1)):
         assert L.dit_debug_linear_i8_tile(*bad) == BAD and b"output tile" in L.dit_last_error()
     try:
-        for t in ((256, 256), (256, 192), (128, 256), (128, 192), (128, 128), (16, 16)):
+        for t in TILES:
             assert L.dit_debug_linear_i8_tile(*t) == B.DIT_OK
-            assert plan(L, 300, 640, 512) == (t if t != (16, 16) else (64, 16))
-        assert plan(L, 4097, 640, 512) != (64, 16)      # more rows than that kernel is launched with
+            assert plan(L, 300, 640, 512) == t
+            assert (plan(L, 4097, 640, 512) == t) == (t[0] >= 128)      # few rows: up to 4,096
     finally:
         assert L.dit_debug_linear_i8_tile(0, 0) == B.DIT_OK
 
@@ -226,7 +229,10 @@ def plan(L, M, N, K, cus=256):
 
 
 def test_the_choice_of_tiles(L):
-    assert plan(L, 1, 5120, 5120) == (16, 16) and plan(L, 17, 5120, 5120) == (32, 16)
+    assert plan(L, 1, 5120, 5120) == (16, 16) and plan(L, 64, 5120, 5120) == (32, 64)
+    assert plan(L, 128, 5120, 13824) == (64, 64) and plan(L, 256, 15360, 5120)[0] >= 128
+    assert {plan(L, M, N, K) for M in (1, 20, 100, 600, 1000, 4000, 30000) for N in (384, 2048, 5120, 15360)
+            for K in (384, 5120, 13824)} >= {(256, 256), (256, 192), (128, 128), (64, 64), (32, 64), (32, 32), (16, 16)}
     assert plan(L, 75600, 15360, 5120) == (256, 256)
     m, n = ctypes.c_int(), ctypes.c_int()
     f = L.dit_debug_linear_i8_plan
