@@ -10,6 +10,8 @@
 //
 // The kernels are bound by memory: a wave holds a row in registers from its one
 // read to its one write (as the norms of 16-bit rows do).
+#include <algorithm>
+
 #include "common.hpp"
 #include "kernels.hpp"
 #include "rows.hpp"
@@ -21,16 +23,21 @@ namespace {
 constexpr float kLeastTop = 127.0f * 0x1p-100f;
 constexpr int64_t kMaxGroups = 1 << 22;   // workgroups of a launch: 2^30 work-items; more rows take turns
 
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+// The wave's index, in a scalar register: so are its row's addresses then.
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+// The largest magnitude so far, NaN once one has been seen (half an instruction a value).
+__device__ __forceinline__ float top_of(float top, float v) { return __builtin_elementwise_maximum(top, fabsf(v)); }
+
+// That of a wave: the bits of infinity and of every NaN are above the finite numbers'.
+__device__ __forceinline__ uint32_t wave_top(float top) {
+  uint32_t v = __float_as_uint(top) & 0x7FFFFFFFu;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, kWave));
   return v;
 }
 
-// How a row is scaled, from the bits of its largest magnitude (those of
-// infinity and of every NaN are above the finite ones).
+// How a row is scaled, from the bits of its largest magnitude.
 struct RowScale {
   float s;        // what is written
   float hi, lo;   // 127 / m in two parts
@@ -81,8 +88,8 @@ __device__ __forceinline__ void store_codes(int8_t* at, const float (&y)[VN], co
 // The largest magnitude of a row held by WPR waves (their workgroup): each has
 // `top` of its part.
 template <int WPR>
-__device__ __forceinline__ uint32_t row_top(uint32_t top) {
-  top = wave_max(top);
+__device__ __forceinline__ uint32_t row_top(float row) {
+  uint32_t top = wave_top(row);
   if constexpr (WPR > 1) {
     __shared__ uint32_t tops[WPR];
     __syncthreads();   // the last row's are read
@@ -103,7 +110,7 @@ __global__ __launch_bounds__(256) void rows_i8_kernel(const T* __restrict__ x, i
   constexpr int VN = Vec16<T>::n, RPW = 4 / WPR;
   const int t = threadIdx.x & (64 * WPR - 1);   // thread of the row
   const int nv = width / VN;
-  for (int64_t row = (int64_t)blockIdx.x * RPW + threadIdx.x / (64 * WPR); row < n_rows; row += (int64_t)gridDim.x * RPW) {
+  for (int64_t row = (int64_t)blockIdx.x * RPW + wave_id() / WPR; row < n_rows; row += (int64_t)gridDim.x * RPW) {
     const T* xr = x + row * x_stride;
     V v[NVL];
 #pragma unroll
@@ -111,13 +118,12 @@ __global__ __launch_bounds__(256) void rows_i8_kernel(const T* __restrict__ x, i
       const int c = t + 64 * WPR * i;
       v[i] = c < nv ? __builtin_nontemporal_load(reinterpret_cast<const V*>(xr + c * VN)) : V{};
     }
-    uint32_t top = 0;
+    float top = 0.f;
 #pragma unroll
     for (int i = 0; i < NVL; ++i)
 #pragma unroll
-      for (int e = 0; e < VN; ++e) top = max(top, magnitude(to_f<T>(v[i][e])));
-    top = row_top<WPR>(top);
-    const RowScale q(top);
+      for (int e = 0; e < VN; ++e) top = top_of(top, to_f<T>(v[i][e]));
+    const RowScale q(row_top<WPR>(top));
     if (t == 0) scales[row] = q.s;
     int8_t* cr = codes + row * codes_stride;
 #pragma unroll
@@ -143,7 +149,7 @@ __global__ __launch_bounds__(256) void rows_i8_wide_kernel(const T* __restrict__
   const int nv = width / VN;
   for (int64_t row = blockIdx.x; row < n_rows; row += gridDim.x) {
     const T* xr = x + row * x_stride;
-    uint32_t top = 0;
+    float top = 0.f;
     for (int c0 = threadIdx.x; c0 < nv; c0 += 256 * U) {
       V v[U];
 #pragma unroll
@@ -154,10 +160,9 @@ __global__ __launch_bounds__(256) void rows_i8_wide_kernel(const T* __restrict__
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < VN; ++e) top = max(top, magnitude(to_f<T>(v[u][e])));
+        for (int e = 0; e < VN; ++e) top = top_of(top, to_f<T>(v[u][e]));
     }
-    top = row_top<4>(top);
-    const RowScale q(top);
+    const RowScale q(row_top<4>(top));
     if (threadIdx.x == 0) scales[row] = q.s;
     int8_t* cr = codes + row * codes_stride;
     for (int c = threadIdx.x; c < nv; c += 256) {
@@ -173,95 +178,102 @@ __global__ __launch_bounds__(256) void rows_i8_wide_kernel(const T* __restrict__
 // A wave's row y [NVL][VN] (zeros behind the row) as codes and scale.
 template <int NVL, int VN>
 __device__ __forceinline__ void emit_codes(const float (&y)[NVL][VN], int lane, int nv, int8_t* cr, float* scale) {
-  uint32_t top = 0;
+  float top = 0.f;
 #pragma unroll
   for (int i = 0; i < NVL; ++i)
 #pragma unroll
-    for (int e = 0; e < VN; ++e) top = max(top, magnitude(y[i][e]));
-  top = wave_max(top);
-  const RowScale q(top);
+    for (int e = 0; e < VN; ++e) top = top_of(top, y[i][e]);
+  const RowScale q(wave_top(top));
   if (lane == 0) *scale = q.s;
 #pragma unroll
   for (int i = 0; i < NVL; ++i)
     if (lane + 64 * i < nv) store_codes<VN, false>(cr + (lane + 64 * i) * VN, y[i], q);
 }
 
-// y = LN(x) (1 + scale) + shift, a row per wave, four rows per workgroup: the
-// statistics and the staging of the request's vectors are those of the kernel
-// that writes y in the rows' own type (layer_norm_mod_kernel), and so is y.
+// y = LN(x) (1 + scale) + shift, a row per wave, four rows per workgroup and
+// turn.  The statistics are those of the kernel that writes y in the rows' own
+// type, in the same order, and so is y.  The workgroups stay resident and keep
+// the vectors of a request in LDS from turn to turn (1 + scale and shift, 8 bytes
+// a column): staged for every four rows, their reads from the L2 were four times
+// the rows' bytes.  A turn over several requests' rows takes one after the other.
+//
+// Workgroups per compute unit (waves per SIMD): what the registers of a row in
+// both forms and what goes with it allow.  LDS holds as many.
 template <typename T, int NVL>
-__global__ __launch_bounds__(256) void modulate_i8_kernel(const T* __restrict__ x, int8_t* __restrict__ codes,
-                                                          float* __restrict__ scales, int64_t n_rows, int hidden, float eps,
-                                                          const float* __restrict__ shift, const float* __restrict__ scale,
-                                                          int64_t mod_stride, ReqTable req) {
+constexpr int modulate_resident() {
+  constexpr int registers = NVL * (4 + Vec16<T>::n) + 35;
+  return registers <= 100 ? 4 : registers <= 160 ? 3 : 2;
+}
+
+template <typename T, int NVL>
+__global__ __launch_bounds__(256, (modulate_resident<T, NVL>())) void modulate_i8_kernel(
+    const T* __restrict__ x, int8_t* __restrict__ codes, float* __restrict__ scales, int64_t n_rows, int hidden, float eps,
+    const float* __restrict__ shift, const float* __restrict__ scale, int64_t mod_stride, ReqTable req) {
   typedef typename Vec16<T>::type V;
   constexpr int VN = Vec16<T>::n, G = VN / 4;
   extern __shared__ f32x4 smod[];   // hidden / 4 vectors of 1 + scale, then of shift: vector G c + g at g nv + c
   const int lane = threadIdx.x & 63;
   const int nv = hidden / VN, h4 = hidden / 4;
+  int kept = -1;                    // the request whose vectors are in LDS
   for (int64_t r0 = (int64_t)blockIdx.x * 4; r0 < n_rows; r0 += (int64_t)gridDim.x * 4) {
-    const int64_t row = r0 + (threadIdx.x >> 6);
-    const int ra = find_req(req.cu, req.n_req, (int)r0);
-    const bool staged = ra == find_req(req.cu, req.n_req, (int)(min(r0 + 4, n_rows) - 1));   // one request's rows
-    __syncthreads();   // the last rows' vectors are read
-    if (staged) {
-      const f32x4* sc = reinterpret_cast<const f32x4*>(scale + (int64_t)ra * mod_stride);
-      const f32x4* sh = reinterpret_cast<const f32x4*>(shift + (int64_t)ra * mod_stride);
-      for (int at = threadIdx.x; at < h4; at += 256) {
-        const int i = G * (at % nv) + at / nv;
-        f32x4 m = sc[i];
+    const int64_t row = min(r0 + wave_id(), n_rows - 1);   // behind the last: the last once more
+    V v[NVL];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) m[u] = 1.0f + m[u];
-        smod[at] = m;
-        smod[h4 + at] = sh[i];
-      }
-      __syncthreads();
+    for (int i = 0; i < NVL; ++i) {
+      const int c = lane + 64 * i;
+      v[i] = c < nv ? __builtin_nontemporal_load(reinterpret_cast<const V*>(x + row * hidden + c * VN)) : V{};
     }
-    if (row >= n_rows) continue;
-    float y[NVL][VN];
-    {
-      V v[NVL];
-      const T* xr = x + row * hidden;
+    const int mine = find_req(req.cu, req.n_req, (int)row);
+    const int last = find_req(req.cu, req.n_req, (int)(min(r0 + 4, n_rows) - 1));
+    for (int r = find_req(req.cu, req.n_req, (int)r0); r <= last; ++r) {   // nearly always one
+      if (req.cu[r + 1] == req.cu[r]) continue;
+      if (r != kept) {
+        kept = r;
+        __syncthreads();   // the former vectors are read
+        const f32x4* sc = reinterpret_cast<const f32x4*>(scale + (int64_t)r * mod_stride);
+        const f32x4* sh = reinterpret_cast<const f32x4*>(shift + (int64_t)r * mod_stride);
+        for (int at = threadIdx.x; at < h4; at += 256) {
+          const int i = G * (at % nv) + at / nv;
+          f32x4 m = sc[i];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) m[u] = 1.0f + m[u];
+          smod[at] = m;
+          smod[h4 + at] = sh[i];
+        }
+        __syncthreads();
+      }
+      if (mine != r) continue;
+      // inside this loop, and hidden from the compiler, which would hold the
+      // row in fp32 beside v and y from before it on
+#pragma unroll
+      for (int i = 0; i < NVL; ++i) asm volatile("" : "+v"(v[i]));
+      float mean, rstd;
+      row_stats<T, NVL>(v, lane, nv, hidden, eps, mean, rstd);
+#pragma unroll
+      for (int i = 0; i < NVL; ++i) asm volatile("" : "+v"(v[i]));
+      float y[NVL][VN];
 #pragma unroll
       for (int i = 0; i < NVL; ++i) {
         const int c = lane + 64 * i;
-        v[i] = c < nv ? __builtin_nontemporal_load(reinterpret_cast<const V*>(xr + c * VN)) : V{};
-      }
-      float mean, rstd;
-      row_stats<T, NVL>(v, lane, nv, hidden, eps, mean, rstd);
-      const int r = staged ? ra : find_req(req.cu, req.n_req, (int)row);
-      const f32x4* sc = reinterpret_cast<const f32x4*>(scale + (int64_t)r * mod_stride);
-      const f32x4* sh = reinterpret_cast<const f32x4*>(shift + (int64_t)r * mod_stride);
-      auto form = [&](auto&& mul_add) {
 #pragma unroll
-        for (int i = 0; i < NVL; ++i) {
-          const int c = lane + 64 * i;
-#pragma unroll
-          for (int e = 0; e < VN; e += 4) {
-            f32x4 m4{}, a4{};
-            if (c < nv) mul_add((c * VN + e) / 4, m4, a4);
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-              y[i][e + u] = c < nv ? fmaf((to_f<T>(v[i][e + u]) - mean) * rstd, m4[u], a4[u]) : 0.f;
+        for (int g = 0; g < G; ++g) {
+          // behind the row, vectors of zeros: y is zero there (or NaN, in a row that has it anyway)
+          f32x4 m4{}, a4{};
+          if (i < NVL - 2 || c < nv) {   // (counts over 8 are rounded up to even ones)
+            m4 = smod[g * nv + c];
+            a4 = smod[h4 + g * nv + c];
           }
-        }
-      };
-      if (staged) {
-        form([&](int j, f32x4& m4, f32x4& a4) {
-          const int at = (j % G) * nv + j / G;
-          m4 = smod[at];
-          a4 = smod[h4 + at];
-        });
-      } else {
-        form([&](int j, f32x4& m4, f32x4& a4) {
-          m4 = sc[j];
-          a4 = sh[j];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) m4[u] = 1.0f + m4[u];
-        });
+          for (int u = 0; u < 4; ++u) y[i][4 * g + u] = fmaf((to_f<T>(v[i][4 * g + u]) - mean) * rstd, m4[u], a4[u]);
+        }
+        // all of the request's vectors asked for at once do not fit the registers: these values before the next ones
+        if (i % 2 == 1) {
+#pragma unroll
+          for (int e = 0; e < VN; ++e) asm volatile("" : "+v"(y[i - 1][e]), "+v"(y[i][e]) :: "memory");
+        }
       }
+      emit_codes<NVL, VN>(y, lane, nv, codes + row * hidden, scales + row);
     }
-    emit_codes<NVL, VN>(y, lane, nv, codes + row * hidden, scales + row);
   }
 }
 
@@ -277,7 +289,7 @@ __global__ __launch_bounds__(256) void add_rms_kernel(const T* x, const T* z, co
   constexpr int VN = Vec16<T>::n;
   const int lane = threadIdx.x & 63;
   const int nv = hidden / VN;
-  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < n_rows; row += (int64_t)gridDim.x * 4) {
+  for (int64_t row = (int64_t)blockIdx.x * 4 + wave_id(); row < n_rows; row += (int64_t)gridDim.x * 4) {
     const int64_t at = row * hidden;
     V v[NVL];
 #pragma unroll
@@ -338,7 +350,7 @@ template <typename T, int NVL>
 hipError_t norm_nvl(const RowsI8Args& p, hipStream_t s) {
   const unsigned grid = groups((p.n_rows + 3) / 4);
   if (p.op == RowOp::kModulate)
-    modulate_i8_kernel<T, NVL><<<grid, 256, (size_t)p.width * 8, s>>>((const T*)p.x, p.codes, p.scales, p.n_rows, p.width,
+    modulate_i8_kernel<T, NVL><<<std::min(grid, (unsigned)(modulate_resident<T, NVL>() * cu_count())), 256, (size_t)p.width * 8, s>>>((const T*)p.x, p.codes, p.scales, p.n_rows, p.width,
                                                                        p.eps, p.shift, p.scale, p.mod_stride, p.req);
   else if (p.op == RowOp::kRms)
     add_rms_kernel<T, NVL><<<grid, 256, 0, s>>>((const T*)p.x, (const T*)p.z, (const T*)p.gain, (T*)p.sum, (T*)p.out,
