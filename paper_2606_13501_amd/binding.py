@@ -434,6 +434,8 @@ def _i8_stream(stream, first, *tensors):
 
 def _vectors(t, name, count, width, stride):
     """A tensor that holds `count` fp32 vectors of `width` values, `stride` values apart, from its address on."""
+    if t.dtype == torch.float32 and t.dim() == 2 and t.stride() == (stride, 1) and t.shape[0] >= count and t.shape[1] >= width:
+        return t   # as most are
     need = ((count - 1) * stride + width) if count else 0
     held = 1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())) if t.numel() else 0
     if t.dtype != torch.float32 or t.stride(-1) != 1 or held < need:

@@ -73,7 +73,9 @@ __device__ __forceinline__ uint32_t codes4(const float* y, const RowScale& q) {
   return q.fine ? lo | hi : 0u;
 }
 
-template <int VN, bool TIES>
+// Past the caches (32,760 rows of 13,824 217 us, 244 without) but for the RMS
+// norm's, which leave with its sums (32,760 x 5,120 176 us, 190 past them).
+template <int VN, bool TIES, bool CACHED = false>
 __device__ __forceinline__ void store_codes(int8_t* at, const float (&y)[VN], const RowScale& q) {
   typename CodeVec<VN>::type o;
   if constexpr (VN == 8) {
@@ -82,7 +84,8 @@ __device__ __forceinline__ void store_codes(int8_t* at, const float (&y)[VN], co
   } else {
     o = codes4<TIES>(y, q);
   }
-  __builtin_nontemporal_store(o, reinterpret_cast<typename CodeVec<VN>::type*>(at));
+  if (CACHED) *reinterpret_cast<typename CodeVec<VN>::type*>(at) = o;
+  else __builtin_nontemporal_store(o, reinterpret_cast<typename CodeVec<VN>::type*>(at));
 }
 
 // The largest magnitude of a row held by WPR waves (their workgroup): each has
@@ -176,7 +179,7 @@ __global__ __launch_bounds__(256) void rows_i8_wide_kernel(const T* __restrict__
 }
 
 // A wave's row y [NVL][VN] (zeros behind the row) as codes and scale.
-template <int NVL, int VN>
+template <int NVL, int VN, bool CACHED>
 __device__ __forceinline__ void emit_codes(const float (&y)[NVL][VN], int lane, int nv, int8_t* cr, float* scale) {
   float top = 0.f;
 #pragma unroll
@@ -187,7 +190,7 @@ __device__ __forceinline__ void emit_codes(const float (&y)[NVL][VN], int lane, 
   if (lane == 0) *scale = q.s;
 #pragma unroll
   for (int i = 0; i < NVL; ++i)
-    if (lane + 64 * i < nv) store_codes<VN, false>(cr + (lane + 64 * i) * VN, y[i], q);
+    if (lane + 64 * i < nv) store_codes<VN, false, CACHED>(cr + (lane + 64 * i) * VN, y[i], q);
 }
 
 // y = LN(x) (1 + scale) + shift, a row per wave, four rows per workgroup and
@@ -198,11 +201,12 @@ __device__ __forceinline__ void emit_codes(const float (&y)[NVL][VN], int lane, 
 // the rows' bytes.  A turn over several requests' rows takes one after the other.
 //
 // Workgroups per compute unit (waves per SIMD): what the registers of a row in
-// both forms and what goes with it allow.  LDS holds as many.
+// both forms and what goes with it allow without spills (at 75,600 x 5,120 with
+// 2, 3 and 4: 202, 232 and 688 us).  LDS holds as many.
 template <typename T, int NVL>
 constexpr int modulate_resident() {
   constexpr int registers = NVL * (4 + Vec16<T>::n) + 35;
-  return registers <= 100 ? 4 : registers <= 160 ? 3 : 2;
+  return registers <= 100 ? 4 : registers <= 140 ? 3 : 2;
 }
 
 template <typename T, int NVL>
@@ -272,7 +276,7 @@ __global__ __launch_bounds__(256, (modulate_resident<T, NVL>())) void modulate_i
           for (int e = 0; e < VN; ++e) asm volatile("" : "+v"(y[i - 1][e]), "+v"(y[i][e]) :: "memory");
         }
       }
-      emit_codes<NVL, VN>(y, lane, nv, codes + row * hidden, scales + row);
+      emit_codes<NVL, VN, false>(y, lane, nv, codes + row * hidden, scales + row);
     }
   }
 }
@@ -340,7 +344,7 @@ __global__ __launch_bounds__(256) void add_rms_kernel(const T* x, const T* z, co
         if (c < nv) __builtin_nontemporal_store(o, reinterpret_cast<V*>(out + at + c * VN));
       }
     }
-    if (codes) emit_codes<NVL, VN>(y, lane, nv, codes + at, scales + row);
+    if (codes) emit_codes<NVL, VN, true>(y, lane, nv, codes + at, scales + row);
   }
 }
 
