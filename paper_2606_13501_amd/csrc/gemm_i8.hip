@@ -55,8 +55,10 @@ template <int AT> __device__ __forceinline__ void load_lds_to(uint32_t lds, int&
 __device__ __forceinline__ void load_lds_16(const u32x4& desc, int voff, int soff) {
   asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" :: "v"(voff), "s"(desc), "s"(soff) : "m0");
 }
+// (A descriptor that the compiler kept in a vector register's lanes comes back
+// right before it: five wait states to a load that reads it.)
 __device__ __forceinline__ void load_lds_4(const u32x4& desc, int voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds), "v"(voff), "s"(desc) : "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" :: "s"(lds), "v"(voff), "s"(desc) : "m0");
 }
 #pragma clang diagnostic pop
 
