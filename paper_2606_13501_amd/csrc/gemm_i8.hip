@@ -44,6 +44,15 @@ __device__ __forceinline__ int32_t sum_of(const i32x4& c, int e) {
   return v;
 }
 
+// gelu_tanh(z) = z / (1 + 2^(z (c0 + c1 z^2))), c0 = -2 log2(e) sqrt(2 / pi), c1 =
+// 0.044715 c0: two multiplications less than step by step (32,760 x 13,824 x
+// 5,120 1,780 -> 1,755 us, in turn).
+__device__ __forceinline__ float gelu(float z) {
+  constexpr float c0 = -2.302208198f, c1 = -0.1029432397f;
+  const float e = __builtin_amdgcn_exp2f(z * fmaf(c1, z * z, c0));   // inf for z << 0: z / inf = 0
+  return z * __builtin_amdgcn_rcpf(1.0f + e);
+}
+
 // A load from global memory into LDS in two parts, an MFMA between them: the
 // address in LDS (m0), then the load itself (16 or 4 bytes a lane).  The vector
 // offset passes through the first part so that it is computed there too.
@@ -461,7 +470,7 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
         for (int e = 0; e < 8; ++e) z[e] = fmaf((float)sum_of(acc[2 * k + e / 4][j], e % 4) * row_scale[j & 1], wscale[k][e], bias[k][e]);
         if constexpr (EPI == DIT_EPI_GELU_TANH) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) z[e] = gelu_tanh(z[e]);
+          for (int e = 0; e < 8; ++e) z[e] = gelu(z[e]);
         } else if constexpr (kRes) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -634,7 +643,7 @@ __global__ __launch_bounds__(64 * S::NW, 1) void gemm_i8_few(
       for (int e = 0; e < 4; ++e) z[e] = fmaf((float)c[e] * sa, sw[e], (float)bias[e]);
       if (EPI == DIT_EPI_GELU_TANH) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = gelu_tanh(z[e]);
+        for (int e = 0; e < 4; ++e) z[e] = gelu(z[e]);
       } else if (EPI == DIT_EPI_RESIDUAL || EPI == DIT_EPI_GATED_RESIDUAL) {
         const V4 r = *reinterpret_cast<const V4*>(ep.res + (int64_t)m * ep.ldr + n);
         if (EPI == DIT_EPI_GATED_RESIDUAL) {
