@@ -261,6 +261,22 @@ def test_add_rms_norm_may_write_its_norm_over_an_input(B):
         assert torch.equal(x3, o)
 
 
+@pytest.mark.parametrize("n,width,dtype", [(1, 8, "bf16"), (6, 24, "bf16"), (5, 1000, "bf16"), (3, 8184, "bf16"),
+                                           (1, 4, "fp32"), (7, 20, "fp32"), (5, 1004, "fp32"), (3, 4092, "fp32")])
+def test_add_rms_norm_without_codes_takes_widths_of_whole_vectors(B, n, width, dtype):
+    """Rows beside each other whose ends lie inside a wave's vectors; the row behind the last stays as it was."""
+    td = TD[dtype]
+    x, z = rows(n, n, width, dtype, 3), rows(n + 50, n, width, dtype, 3)
+    gain = (1 + 0.3 * rows(99, 1, width, dtype)[0]).to(td)
+    sums, outs = torch.full((n + 1, width), 7.0, dtype=td, device="cuda"), torch.full((n + 1, width), 7.0, dtype=td, device="cuda")
+    B.add_rms_norm(x, z, gain, 1e-5, sums[:n], outs[:n])
+    assert torch.equal(sums[:n].cpu(), (x.cpu().float() + z.cpu().float()).to(td))
+    y = R.rms(host(sums[:n]), host(gain), 1e-5)
+    # one rounding to the type: half a step, relative to the value
+    assert (np.abs(host(outs[:n]) - y) <= np.abs(y) * (torch.finfo(td).eps / 2 + E * (N_SUM / 2 + 6))).all()
+    assert bool((sums[n] == 7).all()) and bool((outs[n] == 7).all())
+
+
 def test_add_rms_norm_rows_that_are_not_finite(B):
     x, z = rows(1, 6, 256, "fp32"), rows(2, 6, 256, "fp32")
     x[1, 3], z[2, 0], x[4, 255], z[4, 255] = float("nan"), float("inf"), float("inf"), float("-inf")
