@@ -286,11 +286,11 @@ dit_status dit_debug_attention_plan(const int32_t *cu_q, const int32_t *cu_k, in
  *   m = max(max|y|, 127 * 2^-100),  s = m / 127,  c = 127 y / m to nearest, ties to even,
  * so |c| <= 127 and y = c s within half a step s / 2.  127 y / m is computed to
  * 2^-16 (a value nearer to the middle between two codes may take either); of
- * bf16 rows as they are, exactly.  A row with a value that is not finite gets
- * the scale NaN and codes 0.  A row's codes
- * and scale do not depend on the rows beside it.  Codes are the operands of
- * dit_linear_i8: activations with one scale per token, and weights [out, in]
- * with one per output channel -- their rows -- from the same calls.
+ * bf16 rows as they are and of their RMS norm (which 1 / rms leaves out of y / m),
+ * exactly.  A row with a value that is not finite gets the scale NaN and codes 0.
+ * A row's codes and scale do not depend on the rows beside it.  Codes are the
+ * operands of dit_linear_i8: activations with one scale per token, and weights
+ * [out, in] with one per output channel -- their rows -- from the same calls.
  *
  * codes: int8, rows of a multiple of 16 values, 16-byte aligned.  scales: fp32
  * [n_rows], 4-byte aligned.  What is written must not overlap what is read, but

@@ -23,7 +23,7 @@ namespace dit {
 
 namespace {
 
-constexpr float kLeastTop = 127.0f * 0x1p-100f;
+constexpr float kLeastTop = 127.0f * 0x1p-100f;   // 127 / it = 2^100
 constexpr int64_t kMaxGroups = 1 << 22;   // workgroups of a launch: 2^30 work-items; more rows take turns
 
 // The wave's index, in a scalar register: so are its row's addresses then.
@@ -40,27 +40,30 @@ __device__ __forceinline__ uint32_t wave_top(float top) {
   return v;
 }
 
-// How a row is scaled, from the bits of its largest magnitude.
+// How a row is scaled, from the bits of the largest magnitude of the numbers u
+// that its codes are made from; the row itself is y = u f, 1 <= f < 2.
 struct RowScale {
   float s;        // what is written
-  float hi, lo;   // 127 / m in two parts
+  float hi, lo;   // 127 / m in two parts, m the largest u
   bool fine;      // all values are finite
-  __device__ explicit RowScale(uint32_t top) {
-    const float m = fmaxf(__uint_as_float(top), kLeastTop);
-    fine = top < 0x7F800000u;
-    s = fine ? m / 127.0f : __uint_as_float(0x7FC00000u);
-    hi = 127.0f / m;
-    lo = fmaf(-hi, m, 127.0f) / m;
+  __device__ explicit RowScale(uint32_t top, float f = 1.0f) {
+    const float m = __uint_as_float(top), y = m * f;
+    fine = y <= 0x1.fffffep127f;   // not of a NaN
+    s = fine ? fmaxf(y, kLeastTop) / 127.0f : __uint_as_float(0x7FC00000u);
+    const bool least = y < kLeastTop;
+    hi = least ? f * 0x1p100f : 127.0f / m;
+    lo = least ? 0.0f : fmaf(-hi, m, 127.0f) * hi * (1.0f / 127.0f);
   }
 };
 
 // VN codes as bytes: z + 1.5 x 2^23 leaves z, rounded to nearest even, in the
-// low bits of the sum, two's complement.  The codes of rows as they are (TIES)
-// take z = fl(y hi + y lo), which is 127 y / m rounded once to fp32 but for a
-// part in 2^22 of the step between fp32 numbers: bf16 rows are often exactly in
-// the middle between two codes (127 y / m = k + 1/2 for two numbers of 8 bits),
-// and with 1 / s rounded such values went to either side (1 in 10,000 codes was
-// off by one).  A norm's values are not such numbers: z = y hi inside the sum.
+// low bits of the sum, two's complement.  The codes of rows as they are and of
+// the RMS norm (TIES) take z = fl(y hi + y lo), which is 127 y / m rounded once to
+// fp32 but for a part in 2^22 of the step between fp32 numbers: bf16 rows are often
+// exactly in the middle between two codes (127 y / m = k + 1/2 for two numbers of 8
+// bits, or of 16), and with 1 / s rounded such values went to either side (1 in
+// 10,000 codes was off by one).  The modulated LayerNorm subtracts a mean, which
+// leaves no such numbers but by chance: z = y hi inside the sum.
 template <int VN> struct CodeVec;
 template <> struct CodeVec<8> { typedef u32x2 type; };
 template <> struct CodeVec<4> { typedef uint32_t type; };
@@ -181,19 +184,19 @@ __global__ __launch_bounds__(256) void rows_i8_wide_kernel(const T* __restrict__
   }
 }
 
-// A wave's row y [NVL][VN] (zeros behind the row) as codes and scale.
-template <int NVL, int VN, bool CACHED>
-__device__ __forceinline__ void emit_codes(const float (&y)[NVL][VN], int lane, int nv, int8_t* cr, float* scale) {
+// A wave's row y [NVL][VN] (zeros behind the row) times f as codes and scale.
+template <int NVL, int VN, bool TIES, bool CACHED>
+__device__ __forceinline__ void emit_codes(const float (&y)[NVL][VN], float f, int lane, int nv, int8_t* cr, float* scale) {
   float top = 0.f;
 #pragma unroll
   for (int i = 0; i < NVL; ++i)
 #pragma unroll
     for (int e = 0; e < VN; ++e) top = top_of(top, y[i][e]);
-  const RowScale q(wave_top(top));
+  const RowScale q(wave_top(top), f);
   if (lane == 0) *scale = q.s;
 #pragma unroll
   for (int i = 0; i < NVL; ++i)
-    if (lane + 64 * i < nv) store_codes<VN, false, CACHED>(cr + (lane + 64 * i) * VN, y[i], q);
+    if (lane + 64 * i < nv) store_codes<VN, TIES, CACHED>(cr + (lane + 64 * i) * VN, y[i], q);
 }
 
 // y = LN(x) (1 + scale) + shift, a row per wave, four rows per workgroup and
@@ -279,7 +282,7 @@ __global__ __launch_bounds__(256, (modulate_resident<T, NVL>())) void modulate_i
           for (int e = 0; e < VN; ++e) asm volatile("" : "+v"(y[i - 1][e]), "+v"(y[i][e]) :: "memory");
         }
       }
-      emit_codes<NVL, VN, false>(y, lane, nv, codes + row * hidden, scales + row);
+      emit_codes<NVL, VN, false, false>(y, 1.0f, lane, nv, codes + row * hidden, scales + row);
     }
   }
 }
@@ -288,6 +291,11 @@ __global__ __launch_bounds__(256, (modulate_resident<T, NVL>())) void modulate_i
 // * gain, a row per wave.  The norm is that of the rounded sum, which is what
 // the residual stream goes on with.  sum may be x or z, and out x or z: a row
 // is read by the wave that writes it, before.
+//
+// 1 / rms is a factor of the whole row, so a code is that of sum * gain: a product
+// of two bf16 numbers, which fp32 holds whole (above 2^-126).  Formed from y, whose
+// two roundings move it, half of the values in the middle between two codes (14 in
+// a million) got the odd one.
 template <typename T, int NVL>
 __global__ __launch_bounds__(256) void add_rms_kernel(const T* x, const T* z, const T* __restrict__ gain, T* sum, T* out,
                                                       int8_t* __restrict__ codes, float* __restrict__ scales, int64_t n_rows,
@@ -328,26 +336,34 @@ __global__ __launch_bounds__(256) void add_rms_kernel(const T* x, const T* z, co
         sq = fmaf(f, f, sq);
       }
     const float rs = rsqrtf(wave_sum(sq) / hidden + eps);
-    float y[NVL][VN];
-#pragma unroll
-    for (int i = 0; i < NVL; ++i) {
-      const int c = lane + 64 * i;
-      V g{};
-      if (c < nv) g = *reinterpret_cast<const V*>(gain + c * VN);
-#pragma unroll
-      for (int e = 0; e < VN; ++e) y[i][e] = c < nv ? to_f<T>(v[i][e]) * rs * to_f<T>(g[e]) : 0.f;
-    }
     if (out) {
 #pragma unroll
       for (int i = 0; i < NVL; ++i) {
         const int c = lane + 64 * i;
-        V o;
+        if (c < nv) {
+          const V g = *reinterpret_cast<const V*>(gain + c * VN);
+          V o;
 #pragma unroll
-        for (int e = 0; e < VN; ++e) o[e] = from_f<T>(y[i][e]);
-        if (c < nv) __builtin_nontemporal_store(o, reinterpret_cast<V*>(out + at + c * VN));
+          for (int e = 0; e < VN; ++e) o[e] = from_f<T>(to_f<T>(v[i][e]) * rs * to_f<T>(g[e]));
+          __builtin_nontemporal_store(o, reinterpret_cast<V*>(out + at + c * VN));
+        }
       }
     }
-    if (codes) emit_codes<NVL, VN, true>(y, lane, nv, codes + at, scales + row);
+    if (codes) {
+      // 1 / rms = p f, p a power of two: u = (sum p) gain is exact in bf16.  Behind the row it is zero (or NaN, where p is
+      // not finite and the whole row is not).
+      const float p = __uint_as_float(__float_as_uint(rs) & 0x7F800000u);
+      const float f = __uint_as_float((__float_as_uint(rs) & 0x007FFFFFu) | 0x3F800000u);
+      float u[NVL][VN];
+#pragma unroll
+      for (int i = 0; i < NVL; ++i) {
+        const int c = lane + 64 * i;
+        const V g = c < nv ? *reinterpret_cast<const V*>(gain + c * VN) : V{};
+#pragma unroll
+        for (int e = 0; e < VN; ++e) u[i][e] = to_f<T>(v[i][e]) * p * to_f<T>(g[e]);
+      }
+      emit_codes<NVL, VN, true, true>(u, f, lane, nv, codes + at, scales + row);
+    }
   }
 }
 

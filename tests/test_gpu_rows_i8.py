@@ -327,3 +327,60 @@ def test_streams_graphs_and_two_calls_at_once(B):
             calls(x, z, b)
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) and torch.equal(p, r) for p, q, r in zip(flat(want), flat(a), flat(b)))
+
+
+@pytest.mark.parametrize("add", [True, False])
+def test_codes_of_the_rms_norm_of_bf16_rows_are_exact(B, add):
+    """1 / rms is a factor of the whole row, so a code rounds 127 (s g) / max|s g|, and s g of bf16 numbers has 16 bits.
+    In 64 bits 127 s g is exact and its quotient is rounded once, so rint sees a middle between two codes exactly where
+    there is one; any other quotient z is z / (254 x 65025) from it at least, more than half a step of fp32 at z."""
+    n, width = 300, 5120
+    x, z = rows(21, n, width, "bf16", 3), rows(22, n, width, "bf16", 3)
+    gain = (1 + 0.2 * rows(23, 1, width, "bf16")[0]).bfloat16()
+    total = torch.empty_like(x) if add else None
+    codes, scales = empty_codes(x)
+    B.add_rms_norm(x, z if add else None, gain, 1e-6, total, None, codes, scales)
+    s = host(total if add else x)
+    steps = R.steps(s * host(gain))
+    ties = np.abs(steps) % 1 == 0.5
+    log(f"  {int(ties.sum())} values in the middle between two codes, of {ties.size}")
+    assert ties.sum() >= 5
+    wrong = codes.cpu().numpy() != np.rint(steps).astype(np.int8)
+    assert not wrong.any(), f"{int(wrong.sum())} codes, {int((wrong & ties).sum())} of them ties"
+    both, more = empty_codes(x)
+    out = torch.empty_like(x)
+    B.add_rms_norm(x, z if add else None, gain, 1e-6, total, out, both, more)
+    assert torch.equal(both, codes) and torch.equal(more, scales)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_middles_of_the_rms_norm_go_to_the_even_code(B, dtype):
+    """s = the whole numbers up to 254 and gains of powers of two: 127 y / m = s / 2 exactly."""
+    x = torch.arange(-254, 255, dtype=torch.float32)
+    x = torch.cat([x, x[:3]]).repeat(3, 1) * torch.tensor([[1.0], [2.0 ** -30], [2.0 ** 40]])
+    d = x.to(TD[dtype]).cuda()
+    for g in (1.0, 0.25, -4096.0):
+        gain = torch.full((512,), g, dtype=TD[dtype], device="cuda")
+        codes, scales = empty_codes(d)
+        B.add_rms_norm(d, None, gain, 1e-30, codes=codes, scales=scales)
+        assert torch.equal(codes.cpu(), torch.round(x[0] / 2 * np.sign(g)).to(torch.int8).repeat(3, 1)), g
+        y = R.rms(x.double().numpy(), np.full(512, g), 1e-30)
+        assert np.allclose(host(scales), R.quantum(y), rtol=E * (N_SUM / 2 + 6), atol=0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rms_norm_rows_at_the_ends_of_the_range(B, dtype):
+    """Rows of zeros and of products below the least scale; a norm that passes the largest number in its last factor."""
+    x = torch.zeros(4, 64, dtype=TD[dtype], device="cuda")
+    x[1], x[2], x[3] = 1.0, 3.0, 1.0
+    gain = torch.full((64,), 2.0 ** -110, dtype=TD[dtype], device="cuda")
+    codes, scales = empty_codes(x)
+    B.add_rms_norm(x, None, gain, 1e-6, codes=codes, scales=scales)
+    assert bool((scales == 2.0 ** -100).all()) and bool((codes == 0).all())
+    # y = 1.5 sqrt(64 / 9) x the largest power of two: above the range, though both factors of it are inside
+    x[1], x[1, 9:] = 1.5, 0
+    gain.fill_(2.0 ** 127)
+    out = torch.empty_like(x)
+    B.add_rms_norm(x, None, gain, 1e-6, None, out, codes, scales)
+    assert bool(out[1, :9].isinf().all()) and bool(scales[1].isnan()) and bool((codes[1] == 0).all())
+    assert bool((codes[0] == 0).all()) and bool((codes[2:] == 127).all()) and bool(scales[2:].isfinite().all())
