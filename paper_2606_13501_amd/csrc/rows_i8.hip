@@ -265,16 +265,18 @@ __global__ __launch_bounds__(256, (modulate_resident<T, NVL>())) void modulate_i
 #pragma unroll
       for (int i = 0; i < NVL; ++i) {
         const int c = lane + 64 * i;
+        const bool in = i < NVL - 2 || c < nv;   // (counts over 8 are rounded up to even ones)
+        // behind the row, y is zero: with its mean, mean * rstd times the zeros there may be NaN though no value of the row is
+        const float mu = in ? mean : 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          // behind the row, vectors of zeros: y is zero there (or NaN, in a row that has it anyway)
           f32x4 m4{}, a4{};
-          if (i < NVL - 2 || c < nv) {   // (counts over 8 are rounded up to even ones)
+          if (in) {
             m4 = smod[g * nv + c];
             a4 = smod[h4 + g * nv + c];
           }
 #pragma unroll
-          for (int u = 0; u < 4; ++u) y[i][4 * g + u] = fmaf((to_f<T>(v[i][4 * g + u]) - mean) * rstd, m4[u], a4[u]);
+          for (int u = 0; u < 4; ++u) y[i][4 * g + u] = fmaf((to_f<T>(v[i][4 * g + u]) - mu) * rstd, m4[u], a4[u]);
         }
         // all of the request's vectors asked for at once do not fit the registers: these values before the next ones
         if (i % 2 == 1) {

@@ -384,3 +384,16 @@ def test_rms_norm_rows_at_the_ends_of_the_range(B, dtype):
     B.add_rms_norm(x, None, gain, 1e-6, None, out, codes, scales)
     assert bool(out[1, :9].isinf().all()) and bool(scales[1].isnan()) and bool((codes[1] == 0).all())
     assert bool((codes[0] == 0).all()) and bool((codes[2:] == 127).all()) and bool(scales[2:].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("width", [16, 64, 528, 1040, 2064, 3600])
+def test_adaln_modulate_i8_large_rows_of_one_value(B, width, dtype):
+    """2^112 throughout: the sums and the mean are exact, the deviations 0 and the row is its shift, though 2^112 over the
+    deviation's floor of 1e-6, which a place behind the row could come to, is above the largest number."""
+    x = torch.full((5, width), 2.0 ** 112, dtype=TD[dtype], device="cuda")
+    mod = torch.from_numpy(np.random.default_rng(width).standard_normal((2, 2, width))).float().cuda()
+    codes, scales = empty_codes(x)
+    B.adaln_modulate_i8(x, mod[:, 0], mod[:, 1], 2 * width, [0, 2, 5], 1e-12, codes, scales)
+    sh = host(mod[:, 0])[[0, 0, 1, 1, 1]]
+    check_codes(codes, scales, sh, np.zeros(5), f"shift alone {width} {dtype}")
