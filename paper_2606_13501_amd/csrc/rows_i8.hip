@@ -206,13 +206,15 @@ __device__ __forceinline__ void emit_codes(const float (&y)[NVL][VN], float f, i
 // a column): staged for every four rows, their reads from the L2 were four times
 // the rows' bytes.  A turn over several requests' rows takes one after the other.
 //
-// Workgroups per compute unit (waves per SIMD): what the registers of a row in
-// both forms and what goes with it allow without spills (at 75,600 x 5,120 with
-// 2, 3 and 4: 202, 232 and 688 us).  LDS holds as many.
+// Workgroups per compute unit (waves per SIMD), by the registers of a row in both
+// forms and what goes with it, so that no instance spills (75,600 x 5,120 in bf16
+// with 2, 3 and 4: 249, 233 and 493 us, 15,209 rows of it 58, 54 and 105).  Rows in
+// fp32 lose by the largest number that fits (40,000 x 3,584 with 2 and 3: 121 and
+// 125 us).  LDS holds as many.
 template <typename T, int NVL>
 constexpr int modulate_resident() {
   constexpr int registers = NVL * (4 + Vec16<T>::n) + 35;
-  return registers <= 100 ? 4 : registers <= 140 ? 3 : 2;
+  return registers <= 100 ? 4 : registers <= (sizeof(T) == 2 ? 155 : 140) ? 3 : 2;
 }
 
 template <typename T, int NVL>
@@ -262,9 +264,14 @@ __global__ __launch_bounds__(256, (modulate_resident<T, NVL>())) void modulate_i
 #pragma unroll
       for (int i = 0; i < NVL; ++i) asm volatile("" : "+v"(v[i]));
       float y[NVL][VN];
+      // the lane hidden too: the places in LDS and memory that depend on it would be formed before the rows, all of them,
+      // and spilled in wide rows (40,000 x 8,192 216 us, 173 so)
+      int el = lane;
+      asm volatile("" : "+v"(el));
+      el &= 63;
 #pragma unroll
       for (int i = 0; i < NVL; ++i) {
-        const int c = lane + 64 * i;
+        const int c = el + 64 * i;
         const bool in = i < NVL - 2 || c < nv;   // (counts over 8 are rounded up to even ones)
         // behind the row, y is zero: with its mean, mean * rstd times the zeros there may be NaN though no value of the row is
         const float mu = in ? mean : 0.f;
@@ -284,7 +291,7 @@ __global__ __launch_bounds__(256, (modulate_resident<T, NVL>())) void modulate_i
           for (int e = 0; e < VN; ++e) asm volatile("" : "+v"(y[i - 1][e]), "+v"(y[i][e]) :: "memory");
         }
       }
-      emit_codes<NVL, VN, false, false>(y, 1.0f, lane, nv, codes + row * hidden, scales + row);
+      emit_codes<NVL, VN, false, false>(y, 1.0f, el, nv, codes + row * hidden, scales + row);
     }
   }
 }
