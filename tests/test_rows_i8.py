@@ -240,3 +240,21 @@ def test_the_choice_of_tiles(L):
     assert f(1, 64, 64, 0, ctypes.byref(m), ctypes.byref(n)) == BAD
     assert f(1, 60, 64, 256, ctypes.byref(m), ctypes.byref(n)) == NOT
     assert f(1, 64, 64, 256, None, ctypes.byref(n)) == BAD
+
+
+@pytest.mark.parametrize("last", [2 ** 32 + 4, -2 ** 32 + 4, 2 ** 31])
+@pytest.mark.parametrize("of", [list, np.array, torch.tensor])
+def test_offsets_outside_32_bits_are_refused(of, last):
+    """Cut to 32 bits, [0, 2^32 + 4] would be the offsets of four rows."""
+    i8, f32 = torch.int8, torch.float32
+    cu = of([0, last])
+    mod, scales = _cpu(1, 64, dt=f32), _cpu(4, dt=f32)
+    with pytest.raises(ValueError, match="32-bit"):
+        B.adaln_modulate_i8(_cpu(4, 64), mod, mod, 64, cu, 1e-6, _cpu(4, 64, dt=i8), scales)
+    with pytest.raises(ValueError, match="32-bit"):
+        B.linear_i8(_cpu(4, 64, dt=i8), scales, _cpu(24, 64, dt=i8), _cpu(24, dt=f32), None, _cpu(4, 24), B.EPI_GATED_RESIDUAL,
+                    _cpu(4, 24), _cpu(1, 24, dt=f32), 24, cu)
+    with pytest.raises((ValueError, OverflowError)):
+        B._i32(cu)
+    for fits in ([0, 4], [0, 2 ** 31 - 1], [-2 ** 31, 0]):
+        assert B._i32(of(fits)).tolist() == fits and B._offsets(of(fits)).tolist() == fits
