@@ -333,3 +333,48 @@ def test_the_mlp_of_a_block_in_8_bits(B, rows, D, F):
     assert (np.abs(h(y) - true) <= bound).all()
     rel = np.linalg.norm(h(y) - true) / np.linalg.norm(true - h(x))
     log(f"  MLP {rows} {D} {F}: {rel:.4f} of its result off")
+
+
+TILED = [t for t in TILES if t[0] >= 128]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("epi", ["none", "gelu", "residual", "gated"])
+@pytest.mark.parametrize("M,N,K", [(2100, 8200, 48), (4090, 6152, 256), (1800, 9000, 368), (3000, 7000, 512), (2600, 8200, 624)])
+def test_every_epilogue_and_type_over_several_tiles_of_a_workgroup(B, tile, M, N, K, epi, dtype):
+    """Every tiled shape with more tiles than compute units and K of 1 to 5 steps: an epilogue's stores (twice as many in
+    fp32), its reads of the residual and of the gates of requests that end inside a wave's rows lie between a tile's loads
+    and the next one's waits.  Against the sums in 64 bits on the device, within the roundings counted above; the same bits
+    for every shape and in place."""
+    assert all(-(-M // m) * -(-N // n) > 256 for m, n in TILED)
+    c = Case(B, M, N, K, epi, dtype, [100, 0, 1, M // 2 + 3, M - M // 2 - 104], pad=(16, 0, 8, 16), seed=7)
+    S = (c.a.double() @ c.w.double().T.contiguous()) * c.sa.double()[:, None] * c.sw.double()
+    z = S + c.bias.double()
+    err = E * (2 * S.abs() + z.abs())
+    y = z
+    if epi == "gelu":
+        u = (2 / np.pi) ** 0.5 * (z + 0.044715 * z ** 3)
+        y = 0.5 * z * (1 + torch.tanh(u))
+        # tanh near -1 leaves 2^-53 of z in 1 + tanh
+        err = 1.13 * err + y.abs() * E * (6 * (2 * u).abs().clamp(max=90) + 12) + z.abs() * 2.0 ** -52
+    elif epi == "gated":
+        g = c.gate.double().repeat_interleave(torch.tensor(c.lens, device="cuda"), 0)
+        y, err = z * g, err * g.abs()
+    if c.res is not None:
+        y = c.res.double() + y
+        err = err + E * y.abs()
+    allowed = err + torch.finfo(TD[dtype]).eps / 2 * (y.abs() + err)
+    first = None
+    for t in TILED:
+        tile(*t)
+        c.buf.fill_(7.0)
+        got = c.run().clone()
+        over = (got.double() - y).abs() - allowed
+        assert bool((over <= 0).all()), (t, float(over.max()), divmod(int(over.argmax()), N))
+        first = got if first is None else first
+        assert torch.equal(got, first), t
+        assert c.untouched()
+        if c.res is not None:
+            x = c.res.clone()
+            c.run(x, res=x)
+            assert torch.equal(x, first), t
