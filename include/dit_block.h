@@ -328,7 +328,8 @@ dit_status dit_add_rms_norm(const void *x, const void *z, const void *gain, int6
  * dtype; the epilogues as for dit_linear.  The sum is exact (32-bit integers),
  * the rest fp32, one rounding to dtype at the end: a row of a packed batch has
  * the same bits as alone.  K is a multiple of 16, at most 131,056; N a multiple
- * of 8, at most 2^24; M at most 2^28 (and M N at most 2^44); else DIT_ERR_UNSUPPORTED.  ldo and ldr are at most 2^24.
+ * of 8, at most 2^24; M at most 2^28 and M N at most 2^44; else
+ * DIT_ERR_UNSUPPORTED.  ldo and ldr are at most 2^24.
  * out may be res (the same address and stride). */
 dit_status dit_linear_i8(const int8_t *a, int64_t lda, const float *a_scales, const int8_t *w,
                          int64_t ldw, const float *w_scales, const void *bias, void *out,

@@ -102,6 +102,7 @@ ReqTable single_req(int64_t n_rows) {
 constexpr int kI8MaxStride = 1 << 22;   // a tile's byte offsets stay below 2^30
 constexpr int kI8MaxOut = 1 << 24;      // 16 output rows end below 2^31
 constexpr int kI8MaxRows = 1 << 28;
+constexpr int64_t kI8MaxOutputs = 1ll << 44;
 constexpr int kI8MaxK = 131056;         // 128 * 128 * K stays below 2^31
 
 // Scales need the alignment of their type only: those of some rows begin anywhere.
@@ -137,8 +138,8 @@ dit_status check_linear_i8_size(int64_t M, int N, int K) {
   if (K % 16 || N % 8 || K > kI8MaxK || N > kI8MaxOut)
     return fail(DIT_ERR_UNSUPPORTED, "the 8-bit GEMM needs K %% 16 == 0, K <= %d, N %% 8 == 0 and N <= %d (K=%d N=%d)", kI8MaxK,
                 kI8MaxOut, K, N);
-  // byte offsets of the scales and tile coordinates in 32 bits
-  if (M > kI8MaxRows || (M / 128 + 1) * (N / 128 + 1) > 0x7FFFFFF8ll)
+  // byte offsets of the scales and tile coordinates in 32 bits: at most 2^30 + 2^21 + 2^17 + 1 tiles of 128 x 128
+  if (M > kI8MaxRows || M * N > kI8MaxOutputs)
     return fail(DIT_ERR_UNSUPPORTED, "M=%lld x N=%d outputs are too many tiles", (long long)M, N);
   return DIT_OK;
 }

@@ -258,3 +258,15 @@ def test_offsets_outside_32_bits_are_refused(of, last):
         B._i32(cu)
     for fits in ([0, 4], [0, 2 ** 31 - 1], [-2 ** 31, 0]):
         assert B._i32(of(fits)).tolist() == fits and B._offsets(of(fits)).tolist() == fits
+
+
+def test_the_largest_product(L):
+    """M N = 2^44 is the most; the tiles of every shape then have 32-bit indices."""
+    m, n = ctypes.c_int(), ctypes.c_int()
+    f = lambda M, N: L.dit_debug_linear_i8_plan(M, N, 64, 256, ctypes.byref(m), ctypes.byref(n))
+    for M, N in ((1 << 28, 1 << 16), (1 << 20, 1 << 24), ((1 << 28) - 1, (1 << 16) - 8)):
+        assert f(M, N) == B.DIT_OK
+        for bm, bn in TILES[:5]:
+            assert -(-M // bm) * -(-N // bn) <= 0x7FFFFFF8
+    for M, N in ((1 << 28, (1 << 16) + 8), ((1 << 20) + 1, 1 << 24), (1 << 28, 3 << 15)):
+        assert f(M, N) == NOT and b"too many tiles" in L.dit_last_error()
