@@ -752,8 +752,11 @@ int choose(int64_t M, int N, int K, int cus) {
   return best;
 }
 
-// Tile rows per raster group, as for the bf16 kernel.
-int raster(int tiles_m) { return tiles_m <= 40 ? 8 : tiles_m <= 160 ? 4 : 3; }
+// Tile rows per raster group: of 2, 3, 4 and 8, 4 is the fastest or within 1.1%
+// of it for eleven products of 4 to 296 tile rows, in turn (75,600 x 15,360 x 5,120
+// 4,099, 4,064, 4,048 and 4,126 us, 75,600 x 5,120 x 13,824 3,598, 3,623, 3,594 and
+// 3,718, 15,209 x 15,360 x 5,120 864, 851, 847 and 869).
+constexpr int kRasterRows = 4;
 
 template <typename T>
 Epi<T> epi_of(const LinearI8Args& p) {
@@ -769,7 +772,7 @@ hipError_t launch_tiles(const LinearI8Args& p, int cus, hipStream_t s) {
   const int resident = cus / kXcds * kXcds;
   if (resident >= kXcds && grid > resident) grid = resident;
   gemm_i8_nt<T, EPI, S><<<grid, kThreads, 0, s>>>(p.a, p.lda, p.w, p.ldw, epi_of<T>(p), (int)p.M, p.N, p.K, (int)tiles_m,
-                                                  (int)tiles_n, raster((int)tiles_m));
+                                                  (int)tiles_n, kRasterRows);
   return hipGetLastError();
 }
 

@@ -28,7 +28,7 @@ __device__ __forceinline__ float gelu_tanh(float z) {
 // tiles (the dispatcher places workgroup b on XCD b mod 8); the workgroups of
 // one XCD take its tiles round-robin, so at any time they work on adjacent
 // tiles.  Logical tiles are rastered in groups of group_m tile rows, so the
-// tiles resident on one XCD share A and W panels in its L2 (see raster()).
+// tiles resident on one XCD share A and W panels in its L2.
 struct TileSeq {
   int first, stride, count;   // logical tiles first + stride * it, it < count
   int tiles_m, tiles_n, group_m;
