@@ -59,6 +59,15 @@ namespace {
 constexpr int BK = 64;                              // K step
 static_assert(BK * 2 == kRowBytes, "a step is one cache line of a row");
 
+// gelu_tanh(z) = z (1 + tanh u) / 2 = z / (1 + e^(-2u)), u = sqrt(2/pi) (z + 0.044715 z^3)
+__device__ __forceinline__ float gelu_tanh(float z) {
+  const float k0 = 0.7978845608028654f;  // sqrt(2/pi)
+  const float k1 = 0.044715f;
+  const float u = k0 * fmaf(k1 * z, z * z, z);
+  const float e = __builtin_amdgcn_exp2f(-2.0f * 1.4426950408889634f * u);   // inf for u << 0: z / inf = 0
+  return z * __builtin_amdgcn_rcpf(1.0f + e);
+}
+
 // c += w . a^T for one 16 x 16 block, in place in the accumulation registers.
 // Inline assembly: where registers are left over, the compiler would give the
 // builtin's result other registers than its addend and copy the accumulators

@@ -1,7 +1,6 @@
 // What the tiled GEMM kernels share, whatever their operands' type: the order
 // in which workgroups take output tiles, the loads from global memory straight
-// into LDS, the tile shapes and the GELU of their epilogues.  An operand tile's
-// row is 128 bytes of K per step.
+// into LDS and the tile shapes.  An operand tile's row is 128 bytes of K per step.
 #pragma once
 
 #include "common.hpp"
@@ -14,15 +13,6 @@ constexpr int kWaves = 4;                           // 2 x 2 waves
 constexpr int kThreads = 64 * kWaves;
 constexpr int kRowBytes = 128;                      // one full cache line per tile row and K step
 constexpr int kXcds = 8;                            // gfx950: 8 XCDs, workgroups dispatched round-robin
-
-// gelu_tanh(z) = z (1 + tanh u) / 2 = z / (1 + e^(-2u)), u = sqrt(2/pi) (z + 0.044715 z^3)
-__device__ __forceinline__ float gelu_tanh(float z) {
-  const float k0 = 0.7978845608028654f;  // sqrt(2/pi)
-  const float k1 = 0.044715f;
-  const float u = k0 * fmaf(k1 * z, z * z, z);
-  const float e = __builtin_amdgcn_exp2f(-2.0f * 1.4426950408889634f * u);   // inf for u << 0: z / inf = 0
-  return z * __builtin_amdgcn_rcpf(1.0f + e);
-}
 
 // Tile sequence of a workgroup.  Each XCD owns a contiguous range of logical
 // tiles (the dispatcher places workgroup b on XCD b mod 8); the workgroups of
