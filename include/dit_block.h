@@ -304,6 +304,8 @@ dit_status dit_quantize_rows(const void *x, int64_t x_row_stride, int64_t n_rows
 
 /* dit_adaln_modulate with the result as codes [n_rows, hidden]: the codes of
  * LN(x[i]) * (1 + scale[r]) + shift[r], which is not rounded to dtype before.
+ * The codes of dit_layer_norm_affine are those of one request with its gains
+ * less 1 as scale and its offsets as shift, in fp32.
  * hidden <= 8192 (bf16) or 4096 (fp32), else DIT_ERR_UNSUPPORTED. */
 dit_status dit_adaln_modulate_i8(const void *x, const float *shift, const float *scale,
                                  int64_t mod_stride, const int32_t *cu_seqlens, int n_req,

@@ -397,3 +397,23 @@ def test_adaln_modulate_i8_large_rows_of_one_value(B, width, dtype):
     B.adaln_modulate_i8(x, mod[:, 0], mod[:, 1], 2 * width, [0, 2, 5], 1e-12, codes, scales)
     sh = host(mod[:, 0])[[0, 0, 1, 1, 1]]
     check_codes(codes, scales, sh, np.zeros(5), f"shift alone {width} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_the_affine_layer_norm_as_codes(B, dtype):
+    """One request with the gains less 1 and the offsets in fp32: the norm of layer_norm_affine."""
+    n, width = 37, 1040
+    x, g, b = rows(31, n, width, dtype, 3), rows(32, 1, width, dtype)[0], rows(33, 1, width, dtype)[0]
+    codes, scales = empty_codes(x)
+    B.adaln_modulate_i8(x, b.float()[None], (g.float() - 1)[None], 0, [0, n], 1e-6, codes, scales)
+    h, hg, hb = host(x), host(g), host(b)
+    d = h - h.mean(1, keepdims=True)
+    std = np.sqrt((d * d).mean(1, keepdims=True) + 1e-6)
+    y = d / std * hg + hb
+    # the errors of test_adaln_modulate_i8, and the two roundings of 1 + (g - 1), each up to E of 1 + |g|
+    err = E * (N_SUM * np.abs(h).mean(1) / std[:, 0] * np.abs(hg).max() + (N_SUM / 2 + 8) * (np.abs(y).max(1) + np.abs(hb).max()) +
+               2 * np.abs(d / std).max(1) * (1 + np.abs(hg).max()))
+    check_codes(codes, scales, y, err, f"affine {dtype}")
+    out = torch.empty_like(x)
+    B.layer_norm_affine(x, g, b, 1e-6, out)
+    assert (np.abs(host(out) - y) <= err[:, None] + torch.finfo(x.dtype).eps / 2 * (np.abs(y) + err[:, None])).all()
