@@ -46,7 +46,7 @@ __device__ __forceinline__ int32_t sum_of(const i32x4& c, int e) {
 
 // gelu_tanh(z) = z / (1 + 2^(z (c0 + c1 z^2))), c0 = -2 log2(e) sqrt(2 / pi), c1 =
 // 0.044715 c0: two multiplications less than step by step (32,760 x 13,824 x
-// 5,120 1,780 -> 1,755 us, in turn).
+// 5,120 1.4% faster, in turn).
 __device__ __forceinline__ float gelu(float z) {
   constexpr float c0 = -2.302208198f, c1 = -0.1029432397f;
   const float e = __builtin_amdgcn_exp2f(z * fmaf(c1, z * z, c0));   // inf for z << 0: z / inf = 0
@@ -123,13 +123,13 @@ struct TileWalk {
 // bytes per lane that v_mfma_f32_16x16x32_bf16 takes, in the same time, for
 // twice the products.
 //
-// Large products run at the board's power limit: 75,600 x 15,360 x 5,120 4,171 us,
-// 2.85 PFLOP/s with the matrix cores 77% busy at 1.74 GHz, where a loop of these
+// Large products run at the board's power limit: 75,600 x 15,360 x 5,120 4,068 us,
+// 2.92 PFLOP/s with the matrix cores 78% busy at 1.80 GHz, where a loop of these
 // instructions on registers, random operands, reaches 4.1 PFLOP/s at 2.06 GHz; the
-// bf16 kernel takes 8,404 us.  Three steps a turn of the K loop took 3.8% of the
+// bf16 kernel takes twice as long.  Three steps a turn of the K loop took 3.8% of the
 // cycles away and 2.2% of the time, the clock falling meanwhile.  15,209 x 5,120 x
-// 13,824, gated, 799 us (its 1,200 tiles take five rounds of 256); 32,760 x 13,824
-// x 5,120 with GELU 1,741, without 1,664.
+// 13,824, gated, 784 us (its 1,200 tiles take five rounds of 256); 32,760 x 13,824
+// x 5,120 with GELU 1,675, 75 of them for the GELU (in turn).
 //
 // channel_swizzle: the 16 lanes that read the rows 8 a + 4 h + c of W (a, c = 0
 // .. 3) at one logical chunk touch 16 distinct bank groups: rows of one parity
@@ -513,8 +513,9 @@ __global__ __launch_bounds__(kThreads, 1) void gemm_i8_nt(
 // ring of R turns in LDS for itself, filled straight from global memory in whole
 // cache lines, so the K loop has no barrier, and the ring runs on into the
 // workgroup's next tile while this one's sums are joined.  Bound by the weights'
-// bytes, or by the launch: 1 x 30,720 x 5,120 23.7 us (6.6 TB/s), 64 x 384 x 1,536
-// in fp32 3.9 us.
+// bytes, or by the launch: 1 x 30,720 x 5,120 28.2 us with weights from memory (5.6
+// TB/s) and 23.6 with the same ones again, partly in the last-level cache; 64 x 384
+// x 1,536 in fp32 3.9 us.
 template <int MB_, int NB_, int NW_, int R_>
 struct FewShape {
   static constexpr int MB = MB_, NB = NB_, NW = NW_, R = R_;
@@ -752,11 +753,14 @@ int choose(int64_t M, int N, int K, int cus) {
   return best;
 }
 
-// Tile rows per raster group: of 2, 3, 4 and 8, 4 is the fastest or within 1.1%
-// of it for eleven products of 4 to 296 tile rows, in turn (75,600 x 15,360 x 5,120
-// 4,099, 4,064, 4,048 and 4,126 us, 75,600 x 5,120 x 13,824 3,598, 3,623, 3,594 and
-// 3,718, 15,209 x 15,360 x 5,120 864, 851, 847 and 869).
-constexpr int kRasterRows = 4;
+// Tile rows per raster group: all of them up to 8, so that one XCD reads a tile
+// column's weights (589 x 10,240 x 5,120, 5 tile rows, weights from memory: 41.9
+// us in groups of 4, 40.1 so; read in all, 131 and 77 MB), and 4 of more.  Of 2, 3,
+// 4 and 8, 4 is the fastest or within 1.1% of it for nine products of 16 to 296
+// tile rows, in turn (75,600 x 15,360 x 5,120 4,099, 4,064, 4,048 and 4,126 us,
+// 75,600 x 5,120 x 13,824 3,598, 3,623, 3,594 and 3,718, 15,209 x 15,360 x 5,120
+// 864, 851, 847 and 869).
+int raster(int64_t tiles_m) { return tiles_m <= 8 ? (int)tiles_m : 4; }
 
 template <typename T>
 Epi<T> epi_of(const LinearI8Args& p) {
@@ -772,7 +776,7 @@ hipError_t launch_tiles(const LinearI8Args& p, int cus, hipStream_t s) {
   const int resident = cus / kXcds * kXcds;
   if (resident >= kXcds && grid > resident) grid = resident;
   gemm_i8_nt<T, EPI, S><<<grid, kThreads, 0, s>>>(p.a, p.lda, p.w, p.ldw, epi_of<T>(p), (int)p.M, p.N, p.K, (int)tiles_m,
-                                                  (int)tiles_n, kRasterRows);
+                                                  (int)tiles_n, raster(tiles_m));
   return hipGetLastError();
 }
 

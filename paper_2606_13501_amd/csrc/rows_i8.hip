@@ -10,9 +10,11 @@
 //
 // The kernels are bound by memory: a wave holds a row in registers from its one
 // read to its one write (as the norms of 16-bit rows do).  In bf16, bytes in and
-// out: modulated 75,600 x 5,120 202 us (5.8 TB/s) and 15,209 x 5,120 of four
-// requests 56 us (4.2); sums and their RMS norm 32,760 x 5,120 186 us (6.3); rows
-// of 13,824, 32,760 of them, 220 us (6.2).
+// out: modulated 75,600 x 5,120 206 us (5.6 TB/s) and 15,209 x 5,120 of four
+// requests 52 us (4.5); sums and their RMS norm 32,760 x 5,120 184 us (6.4); rows
+// of 13,824, 32,760 of them, 220 us (6.2).  These with other work between the
+// calls; the comparisons below are of calls in a row, whose times differ from them
+// by -3% to 15%.
 #include <algorithm>
 
 #include "common.hpp"
@@ -79,8 +81,8 @@ __device__ __forceinline__ uint32_t codes4(const float* y, const RowScale& q) {
   return q.fine ? lo | hi : 0u;
 }
 
-// Past the caches (32,760 rows of 13,824 217 us, 244 without) but for the RMS
-// norm's, which leave with its sums (32,760 x 5,120 176 us, 190 past them).
+// Past the caches (32,760 rows of 13,824 215 us, 244 without) but for the RMS
+// norm's, which leave with its sums (32,760 x 5,120 183 us, 192 past them).
 template <int VN, bool TIES, bool CACHED = false>
 __device__ __forceinline__ void store_codes(int8_t* at, const float (&y)[VN], const RowScale& q) {
   typename CodeVec<VN>::type o;
@@ -208,7 +210,7 @@ __device__ __forceinline__ void emit_codes(const float (&y)[NVL][VN], float f, i
 //
 // Workgroups per compute unit (waves per SIMD), by the registers of a row in both
 // forms and what goes with it, so that no instance spills (75,600 x 5,120 in bf16
-// with 2, 3 and 4: 249, 233 and 493 us, 15,209 rows of it 58, 54 and 105).  Rows in
+// with 2, 3 and 4: 250, 235 and 493 us, 15,209 rows of it 58, 54 and 105).  Rows in
 // fp32 lose by the largest number that fits (40,000 x 3,584 with 2 and 3: 121 and
 // 125 us).  LDS holds as many.
 template <typename T, int NVL>
