@@ -124,7 +124,7 @@ struct TileWalk {
 // twice the products.
 //
 // Large products run at the board's power limit: 75,600 x 15,360 x 5,120 4,068 us,
-// 2.92 PFLOP/s with the matrix cores 78% busy at 1.80 GHz, where a loop of these
+// 2.92 PFLOP/s with the matrix cores 78% busy at 1.78 GHz, where a loop of these
 // instructions on registers, random operands, reaches 4.1 PFLOP/s at 2.06 GHz; the
 // bf16 kernel takes twice as long.  Three steps a turn of the K loop took 3.8% of the
 // cycles away and 2.2% of the time, the clock falling meanwhile.  15,209 x 5,120 x
